@@ -15,6 +15,10 @@
  *   mf_schedule_round    the two steps back to back (one call per round)
  *   mf_*_typed           the same with one predictor per GPU type
  *   mf_schedule_round_update  the next periodic round: re-scores what changed
+ *   mf_predictor_loss    the predictor's loss over profiled pairs, with every gradient
+ *   mf_predict_pairs     its predictions for listed pairs
+ *   mf_layer_norm, mf_layer_norm_grad, mf_dropout   the layers these are made of, for
+ *                        predictors of other shapes
  *
  * Conventions shared by every call
  *   - Pointers named d_* are DEVICE pointers (HIP global memory on the device
@@ -36,7 +40,9 @@
  *     stream, or a synchronisation of it, orders after them); every call
  *     that takes an mf_result *h_res (required, not NULL) steers its
  *     iteration from the host, waits for its own work and fills *h_res.
- *     mf_check_certificate_noalloc takes its own stream and never waits.
+ *     mf_check_certificate_noalloc takes its own stream and never waits, and so
+ *     do the calls on predictors and layers at the end of this file: they only
+ *     enqueue kernels, so a HIP graph can capture them.
  *   - Return value: MF_OK (0) or a negative MF_ERR_* code; nothing is thrown
  *     across this boundary.  On error the output buffers are unspecified.
  *   - A context may be used by one thread at a time.
@@ -90,6 +96,12 @@ typedef struct mf_ctx mf_ctx;
  * slowdown of the online workload of the pair as a fraction in (0, 1); a pair
  * whose prediction exceeds slow_limit is infeasible like one that does not fit
  * in memory.
+ * Optional layer norm: the features are metrics in different units; with
+ * d_ln_w not NULL each workload's F features are normalised before layer 1,
+ *   x'_f = (x_f - mean) / sqrt(variance + ln_eps) * d_ln_w[f] + d_ln_b[f]
+ * with the mean and the (biased) variance of that workload's features, entries
+ * [0,F) of the two vectors for the online and [F,2F) for the offline one.
+ * The memory fraction and the SM share are taken from the features as they are.
  * All parameter pointers are DEVICE pointers to float32, row-major.
  */
 typedef struct {
@@ -110,6 +122,9 @@ typedef struct {
     const float *d_W3_slow;     /* [H] or NULL: output weights of the slowdown unit     */
     const float *d_b3_slow;     /* [1]  (with d_W3_slow)                                */
     float   slow_limit;         /* pairs predicted above it are infeasible              */
+    const float *d_ln_w;        /* [2F] or NULL: weight of the norm of the features     */
+    const float *d_ln_b;        /* [2F]  (with d_ln_w)                                  */
+    float   ln_eps;             /* > 0                                                  */
 } mf_predictor;
 
 /* Filled on the host by the solving calls. */
@@ -379,6 +394,114 @@ int mf_last_timings(mf_ctx *ctx, float what[16]);
  * instruction of the default scoring path); out[6], out[7] = 0.  Waits for the stream.
  */
 int mf_measure_ceilings(mf_ctx *ctx, const void *d_buffer, int64_t bytes, float out[8]);
+
+/*
+ * ---- Fitting a predictor, and its layers ----
+ *
+ * The calls below only enqueue kernels on the context's stream, never wait
+ * and may be captured into a HIP graph, with any eager work of the context
+ * ordered before or after the graph (they share the context's 0.3 MB
+ * scratch of folded weights).  They are not bound to the context's max_n x max_m.
+ */
+
+/*
+ * A dropout: each element is kept with probability 1 - p, independently, and
+ * then multiplied by the inverse of the kept share.  Which ones are kept
+ * follows from (seed, step, layer, index of the element) alone, by Philox 4x32
+ * with ten rounds: the mask is never stored, and the same call on the
+ * gradient is the backward pass.  Element e takes the 16 bits number e % 8
+ * (least significant half of the first word first) of the block with
+ * key (seed, seed >> 32) and
+ * counter (g, g >> 32 | layer << 16, step, step >> 32), g = e / 8, and is kept
+ * where they are at least T = round-half-even(65536 p); what is kept is
+ * multiplied by 65536 / (65536 - T) in float32.  0 <= p < 1, T < 65536.
+ * With d_step not NULL the step is read from there (device, 8-byte aligned) when the
+ * kernels run, so that a captured training step has a new mask in every replay.
+ */
+typedef struct {
+    float    p;
+    uint64_t seed, step;
+    const uint64_t *d_step;
+} mf_dropout_rule;
+
+/* Types of the layers' values.  Weights and their gradients are float32. */
+enum { MF_F32 = 0, MF_F16 = 1, MF_BF16 = 2 };
+
+/*
+ * y = (x - mean) / sqrt(variance + eps) * w + b for each of `rows` rows of
+ * `width` values (1..8192, else MF_ERR_SHAPE), rows ldx and ldy values apart (>= width).  Statistics in float32,
+ * one rounding to the type.  Rows may begin at any multiple of the type's
+ * size.  d_y may be d_x with ldy = ldx; else they must not overlap.
+ */
+int mf_layer_norm(mf_ctx *ctx, int type, const void *d_x, int64_t rows, int64_t width, int64_t ldx,
+                  const float *d_w, const float *d_b, float eps, void *d_y, int64_t ldy);
+
+/*
+ * Its gradients: d_dx [rows][width], d_dw and d_db [width] float32 (summed over rows
+ * in a fixed order: the same call gives the same bits).  The mean and the variance are taken from d_x again.
+ * d_dx may be d_x or d_dy (same pitch).  d_work: 16-byte aligned device memory of
+ * mf_layer_norm_grad_work(...) bytes at least (that call returns a negative code
+ * for arguments this one would refuse); it may hold anything.  With rows = 0 d_dw and d_db are zero.
+ */
+int64_t mf_layer_norm_grad_work(mf_ctx *ctx, int64_t rows, int64_t width);
+int mf_layer_norm_grad(mf_ctx *ctx, int type, const void *d_x, int64_t rows, int64_t width, int64_t ldx,
+                       const void *d_dy, int64_t lddy, const float *d_w, float eps, void *d_dx, int64_t lddx,
+                       float *d_dw, float *d_db, void *d_work, int64_t work_bytes);
+
+/*
+ * Dropout of rows of values; element e = row * width + column whatever the
+ * pitches.  `layer` (0..65535) tells dropouts of one step apart.  What is dropped
+ * is zero whatever it was, a NaN or infinity too.  d_y may be d_x with ldy = ldx.
+ */
+int mf_dropout(mf_ctx *ctx, int type, const void *d_x, int64_t rows, int64_t width, int64_t ldx,
+               const mf_dropout_rule *rule, int layer, void *d_y, int64_t ldy);
+
+/*
+ * Pairs somebody has profiled: online workload d_on[s] (a row of the online features)
+ * beside offline workload d_off[s] reached d_target[s] of its throughput, and slowed the
+ * online one down by d_target_slow[s].  A sample with an index out of range (-1, say)
+ * names no pair: it fills a batch up and has no part in anything.  A target that is a
+ * NaN was not measured and has no part in the loss.
+ */
+typedef struct {
+    const int32_t *d_on, *d_off;        /* [count]                                      */
+    const float *d_target;              /* [count]                                      */
+    const float *d_target_slow;         /* [count] with the slowdown unit, else NULL    */
+    int64_t count;
+} mf_samples;
+
+/* Where gradients go (device, float32), shaped like the parameters of mf_predictor;
+ * members of parts the predictor does not have are ignored. */
+typedef struct {
+    float *d_W1, *d_b1, *d_W2, *d_b2, *d_W3, *d_b3, *d_W1sm, *d_W3_slow, *d_b3_slow, *d_ln_w, *d_ln_b;
+} mf_gradients;
+
+/*
+ * The predictor's loss over the samples and its gradients (paper: Section
+ * "Implementation", predictors are trained on profiled pairs):
+ *   *d_loss = scale * (sum over s of (sigma_s - d_target[s])^2 + the same of the slowdown unit).
+ * scale is the caller's, 1 / count for a mean.  With a dropout (else NULL) both hidden layers are dropped
+ * out after their ReLU: hidden unit k of sample s is element s * H + k of layer 0
+ * (the first) or 1.  grads may be NULL: the loss alone, as for validation.
+ * d_sigma and d_sigma_slow ([count], either may be NULL) receive the predictions, with the same dropout; 0 for a
+ * sample that names no pair.  Gradients are sums in a fixed order: the same call gives the same bits.
+ * A ReLU passes no gradient at 0.  d_work as in mf_layer_norm_grad.
+ * scale, mem_feature, mem_limit and slow_limit of the predictor play no part but have to be valid.
+ */
+int64_t mf_predictor_loss_work(mf_ctx *ctx, const mf_predictor *pred, int64_t count);
+int mf_predictor_loss(mf_ctx *ctx, const mf_predictor *pred, const float *d_on, int n, const float *d_off, int m,
+                      const mf_samples *samples, const mf_dropout_rule *dropout, float scale,
+                      const mf_gradients *grads, float *d_loss, float *d_sigma, float *d_sigma_slow,
+                      void *d_work, int64_t work_bytes);
+
+/*
+ * Predictions for `count` listed pairs: d_sigma[s] (and d_sigma_slow[s], may be NULL) is
+ * what mf_score_pairs would give as the score of online workload d_pair_on[s] and offline workload d_pair_off[s], to within rounding,
+ * or 0 where an index is out of range.  Whether a pair fits in memory plays no part.
+ */
+int mf_predict_pairs(mf_ctx *ctx, const mf_predictor *pred, const float *d_on, int n, const float *d_off, int m,
+                     const int32_t *d_pair_on, const int32_t *d_pair_off, int64_t count,
+                     float *d_sigma, float *d_sigma_slow);
 
 const char *mf_strerror(int code);
 const char *mf_last_hip_error(mf_ctx *ctx);

@@ -20,7 +20,8 @@ FALLBACK_TEAMS, FALLBACK_SEARCHES = 1, 2
 EXPORTS = ["mf_create", "mf_destroy", "mf_score_pairs", "mf_solve_assignment",
            "mf_check_certificate", "mf_check_certificate_noalloc", "mf_schedule_round", "mf_schedule_round_update", "mf_score_pairs_typed",
            "mf_schedule_round_typed", "mf_set_option", "mf_last_timings", "mf_measure_ceilings",
-           "mf_strerror", "mf_last_hip_error"]
+           "mf_predictor_loss", "mf_predictor_loss_work", "mf_predict_pairs", "mf_layer_norm", "mf_layer_norm_grad",
+           "mf_layer_norm_grad_work", "mf_dropout", "mf_strerror", "mf_last_hip_error"]
 
 TIMING_NAMES = ["projections_ms", "pair_scoring_ms", "bulk_bid_ms", "bulk_bid_launches",
                 "prepare_ms", "duals_ms", "certificate_ms", "auction_ms", "bulk_bid_bytes",
@@ -33,7 +34,29 @@ class Predictor(C.Structure):
                 ("d_W1", C.c_void_p), ("d_b1", C.c_void_p), ("d_W2", C.c_void_p),
                 ("d_b2", C.c_void_p), ("d_W3", C.c_void_p), ("d_b3", C.c_void_p),
                 ("d_W1sm", C.c_void_p), ("sm_on_feature", C.c_int32), ("sm_off_feature", C.c_int32),
-                ("d_W3_slow", C.c_void_p), ("d_b3_slow", C.c_void_p), ("slow_limit", C.c_float)]
+                ("d_W3_slow", C.c_void_p), ("d_b3_slow", C.c_void_p), ("slow_limit", C.c_float),
+                ("d_ln_w", C.c_void_p), ("d_ln_b", C.c_void_p), ("ln_eps", C.c_float)]
+
+
+class DropoutRule(C.Structure):
+    _fields_ = [("p", C.c_float), ("seed", C.c_uint64), ("step", C.c_uint64), ("d_step", C.c_void_p)]
+
+
+class Samples(C.Structure):
+    _fields_ = [("d_on", C.c_void_p), ("d_off", C.c_void_p), ("d_target", C.c_void_p), ("d_target_slow", C.c_void_p),
+                ("count", C.c_int64)]
+
+
+# members of mf_gradients and the names their parameters have in a predictor's dictionary
+PARAMETERS = (("d_W1", "W1"), ("d_b1", "b1"), ("d_W2", "W2"), ("d_b2", "b2"), ("d_W3", "W3"), ("d_b3", "b3"),
+              ("d_W1sm", "W1sm"), ("d_W3_slow", "W3slow"), ("d_b3_slow", "b3slow"), ("d_ln_w", "ln_w"), ("d_ln_b", "ln_b"))
+
+
+class Gradients(C.Structure):
+    _fields_ = [(member, C.c_void_p) for member, _ in PARAMETERS]
+
+
+LAYER_TYPES = {torch.float32: 0, torch.float16: 1, torch.bfloat16: 2}
 
 
 class Result(C.Structure):
@@ -78,6 +101,15 @@ def load_library():
     lib.mf_schedule_round_typed.argtypes = [vp, C.POINTER(Predictor), i32, vp, vp, i32, vp, i32, vp, i64, vp, vp, vp,
                                             C.POINTER(Result)]
     lib.mf_measure_ceilings.argtypes = [vp, vp, i64, C.POINTER(C.c_float * 8)]
+    pred, f32 = C.POINTER(Predictor), C.c_float
+    lib.mf_predictor_loss.argtypes = [vp, pred, vp, i32, vp, i32, C.POINTER(Samples), C.POINTER(DropoutRule), f32,
+                                      C.POINTER(Gradients), vp, vp, vp, vp, i64]
+    lib.mf_predictor_loss_work.argtypes = [vp, pred, i64]
+    lib.mf_predict_pairs.argtypes = [vp, pred, vp, i32, vp, i32, vp, vp, i64, vp, vp]
+    lib.mf_layer_norm.argtypes = [vp, i32, vp, i64, i64, i64, vp, vp, f32, vp, i64]
+    lib.mf_layer_norm_grad.argtypes = [vp, i32, vp, i64, i64, i64, vp, i64, vp, f32, vp, i64, vp, vp, vp, i64]
+    lib.mf_layer_norm_grad_work.argtypes = [vp, i64, i64]
+    lib.mf_dropout.argtypes = [vp, i32, vp, i64, i64, i64, C.POINTER(DropoutRule), i32, vp, i64]
     lib.mf_set_option.argtypes = [vp, C.c_char_p, i64]
     lib.mf_last_timings.argtypes = [vp, C.POINTER(C.c_float * 16)]
     lib.mf_strerror.argtypes = [i32]
@@ -86,7 +118,7 @@ def load_library():
     lib.mf_last_hip_error.restype = C.c_char_p
     for name in EXPORTS:
         if name not in ("mf_strerror", "mf_last_hip_error"):
-            getattr(lib, name).restype = i32
+            getattr(lib, name).restype = i64 if name.endswith("_work") else i32
     return lib
 
 
@@ -134,11 +166,135 @@ class Context:
             raise MuxmatchError(rc, detail)
         return rc
 
-    def predictor(self, params, scale, mem_feature=0, mem_limit=1.0, sm=None, slow_limit=None):
+    def _flat(self, t, dtype, count, what, optional=False):
+        """Pointer of a contiguous tensor of `count` values on this context's device."""
+        if t is None and optional:
+            return None
+        if not isinstance(t, torch.Tensor) or not t.is_cuda or t.device.index != self.device or t.dtype != dtype or not t.is_contiguous():
+            raise TypeError(f"{what}: expected a contiguous tensor of {dtype} on device {self.device}")
+        if t.numel() != count:
+            raise ValueError(f"{what}: expected {count} values, got {t.numel()}")
+        return t.data_ptr() or None
+
+    def _rows(self, t, like, what):
+        """(pointer, pitch) of a matrix whose rows may lie apart but whose values lie side by side."""
+        if not isinstance(t, torch.Tensor) or not t.is_cuda or t.device.index != self.device or t.dtype not in LAYER_TYPES or t.dim() != 2:
+            raise TypeError(f"{what}: expected a float32, float16 or bfloat16 matrix on device {self.device}")
+        if like is not None and (t.dtype != like.dtype or t.shape != like.shape):
+            raise ValueError(f"{what}: expected a matrix of the input's shape and type")
+        rows, width = t.shape
+        pitch = t.stride(0) if rows > 1 else max(width, 1)
+        if (width > 1 and t.stride(1) != 1) or pitch < width:
+            raise ValueError(f"{what}: the values of a row have to lie side by side, rows must not overlap")
+        return t.data_ptr() or None, pitch
+
+    def _work(self, work, needed):
+        """The caller's scratch, or as much from torch's allocator, in the order of this context's stream."""
+        if needed < 0:
+            raise MuxmatchError(int(needed))
+        if work is None:
+            with torch.cuda.stream(self.stream):
+                work = torch.empty(max(int(needed), 16), dtype=torch.uint8, device=f"cuda:{self.device}")
+        elif not isinstance(work, torch.Tensor) or not work.is_cuda or work.device.index != self.device or work.dtype != torch.uint8 or not work.is_contiguous():
+            raise TypeError(f"work: expected a contiguous tensor of torch.uint8 on device {self.device}")
+        return work
+
+    def _dropout(self, p, seed, step):
+        rule = DropoutRule(float(p), int(seed) & (2 ** 64 - 1), 0, None)
+        if isinstance(step, torch.Tensor):
+            rule.d_step = self._flat(step, torch.int64, 1, "step")
+        else:
+            rule.step = int(step) & (2 ** 64 - 1)
+        return rule
+
+    def layer_norm(self, x, weight, bias, y, eps=1e-5):
+        """y = layer norm of the rows of x (float32, float16 or bfloat16; weight and bias float32).  y may be x."""
+        (px, ldx), (py, ldy) = self._rows(x, None, "x"), self._rows(y, x, "y")
+        rows, width = x.shape
+        self._check(_lib.mf_layer_norm(self._h, LAYER_TYPES[x.dtype], px, rows, width, ldx,
+                                       self._flat(weight, torch.float32, width, "weight"),
+                                       self._flat(bias, torch.float32, width, "bias"), float(eps), py, ldy))
+
+    def layer_norm_grad_work(self, rows, width):
+        """Bytes of scratch layer_norm_grad needs."""
+        needed = _lib.mf_layer_norm_grad_work(self._h, int(rows), int(width))
+        if needed < 0:
+            raise MuxmatchError(int(needed))
+        return int(needed)
+
+    def layer_norm_grad(self, x, dy, weight, dx, dweight, dbias, eps=1e-5, work=None):
+        """dx, dweight and dbias of layer_norm from dy.  dx may be x or dy."""
+        (px, ldx), (pdy, lddy), (pdx, lddx) = self._rows(x, None, "x"), self._rows(dy, x, "dy"), self._rows(dx, x, "dx")
+        rows, width = x.shape
+        work = self._work(work, _lib.mf_layer_norm_grad_work(self._h, rows, width))
+        flat = lambda t, what: self._flat(t, torch.float32, width, what)
+        self._check(_lib.mf_layer_norm_grad(self._h, LAYER_TYPES[x.dtype], px, rows, width, ldx, pdy, lddy,
+                                            flat(weight, "weight"), float(eps), pdx, lddx, flat(dweight, "dweight"),
+                                            flat(dbias, "dbias"), work.data_ptr(), work.numel()))
+
+    def dropout(self, x, y, p, seed, step=0, layer=0):
+        """y = dropout of x, the mask made from (seed, step, layer, element); on a gradient, the backward pass.
+        step: a number, or an int64 tensor of one value on the device.  y may be x."""
+        (px, ldx), (py, ldy) = self._rows(x, None, "x"), self._rows(y, x, "y")
+        rule = self._dropout(p, seed, step)
+        self._check(_lib.mf_dropout(self._h, LAYER_TYPES[x.dtype], px, x.shape[0], x.shape[1], ldx, C.byref(rule),
+                                    int(layer), py, ldy))
+
+    def _sides(self, pred, x_on, x_off):
+        """Features of both sides: [n, F] and [m, F]."""
+        out = []
+        for x, what in ((x_on, "x_on"), (x_off, "x_off")):
+            if not isinstance(x, torch.Tensor) or x.dim() != 2 or x.shape[1] != pred.F:
+                raise ValueError(f"{what}: expected a matrix of {pred.F} features a workload")
+            out += [self._flat(x, torch.float32, x.numel(), what), x.shape[0]]
+        return out
+
+    def predictor_loss_work(self, pred, count):
+        """Bytes of scratch predictor_loss needs."""
+        needed = _lib.mf_predictor_loss_work(self._h, C.byref(pred), int(count))
+        if needed < 0:
+            raise MuxmatchError(int(needed))
+        return int(needed)
+
+    def predictor_loss(self, pred, x_on, x_off, on, off, target, loss, grads=None, target_slow=None, dropout=None,
+                       scale=None, sigma=None, sigma_slow=None, work=None):
+        """loss[0] = scale * sum of squared errors of the predictions for the pairs (on[s], off[s]), and in `grads`, a
+        dictionary of tensors shaped like the predictor's parameters, its gradients.  on, off: int32, out of range
+        (-1) for samples that only fill the batch; target: float32, NaN where not measured.  dropout: (p, seed) or
+        (p, seed, step).  scale: 1 / number of samples if not given."""
+        count = on.numel() if isinstance(on, torch.Tensor) else 0
+        flat = lambda t, what: self._flat(t, torch.float32, count, what, optional=True)
+        sides = self._sides(pred, x_on, x_off)
+        samples = Samples(self._flat(on, torch.int32, count, "on"), self._flat(off, torch.int32, count, "off"),
+                          self._flat(target, torch.float32, count, "target"), flat(target_slow, "target_slow"), count)
+        rule = self._dropout(*dropout, *((0,) if len(dropout) == 2 else ())) if dropout is not None else None
+        if grads is not None:
+            pointers = []
+            for member, name in PARAMETERS:
+                has = getattr(pred, member) is not None
+                pointers.append(self._flat(grads[name], torch.float32, pred._keep[name].numel(), f"grads[{name!r}]") if has else None)
+            grads = Gradients(*pointers)
+        work = self._work(work, _lib.mf_predictor_loss_work(self._h, C.byref(pred), count))
+        self._check(_lib.mf_predictor_loss(
+            self._h, C.byref(pred), *sides, C.byref(samples), C.byref(rule) if rule is not None else None,
+            1.0 / max(count, 1) if scale is None else float(scale), C.byref(grads) if grads is not None else None,
+            self._flat(loss, torch.float32, 1, "loss"), flat(sigma, "sigma"), flat(sigma_slow, "sigma_slow"),
+            work.data_ptr(), work.numel()))
+
+    def predict_pairs(self, pred, x_on, x_off, on, off, sigma, sigma_slow=None):
+        """sigma[s] (and sigma_slow[s]) = what the predictor says of the pair (on[s], off[s])."""
+        count = on.numel() if isinstance(on, torch.Tensor) else 0
+        self._check(_lib.mf_predict_pairs(
+            self._h, C.byref(pred), *self._sides(pred, x_on, x_off), self._flat(on, torch.int32, count, "on"),
+            self._flat(off, torch.int32, count, "off"), count, self._flat(sigma, torch.float32, count, "sigma"),
+            self._flat(sigma_slow, torch.float32, count, "sigma_slow", optional=True)))
+
+    def predictor(self, params, scale, mem_feature=0, mem_limit=1.0, sm=None, slow_limit=None, norm_eps=None):
         """params: dict of float32 device tensors W1 [H,2F], b1, W2 [H,H], b2, W3 [H], b3 [1];
         with sm = (online feature, offline feature) also W1sm [H], the weights of the
         pair-dependent SM input; with slow_limit also W3slow [H], b3slow [1], the second output
-        unit that predicts the online workload's slowdown (pairs above slow_limit are infeasible)."""
+        unit that predicts the online workload's slowdown (pairs above slow_limit are infeasible);
+        with norm_eps also ln_w [2F], ln_b [2F], weight and bias of the layer norm of the features."""
         H = params["b1"].numel()
         F = params["W1"].shape[1] // 2
         p = Predictor(F, H, float(scale), int(mem_feature), float(mem_limit),
@@ -147,7 +303,10 @@ class Context:
                       0 if sm is None else int(sm[0]), 0 if sm is None else int(sm[1]),
                       _ptr(params["W3slow"], torch.float32) if slow_limit is not None else None,
                       _ptr(params["b3slow"], torch.float32) if slow_limit is not None else None,
-                      0.0 if slow_limit is None else float(slow_limit))
+                      0.0 if slow_limit is None else float(slow_limit),
+                      _ptr(params["ln_w"], torch.float32) if norm_eps is not None else None,
+                      _ptr(params["ln_b"], torch.float32) if norm_eps is not None else None,
+                      0.0 if norm_eps is None else float(norm_eps))
         p._keep = params
         return p
 

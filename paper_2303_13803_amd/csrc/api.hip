@@ -1,5 +1,6 @@
 // C entry points: argument checks, context life cycle, stage timing.
 #include "internal.h"
+#include <math.h>
 #include <stdlib.h>
 #include <string.h>
 #include <new>
@@ -13,14 +14,9 @@ template <typename T> hipError_t dev_alloc(T **p, size_t count)
 
 bool aligned16(const void *p) { return ((uintptr_t)p & 15u) == 0; }
 
-int check_matrix(const mf_ctx *ctx, const void *d_W, int n, int m, int64_t ldw)
-{
-    if (!ctx || !d_W || n <= 0 || m <= 0 || ldw < m || (ldw & 3) || !aligned16(d_W)) return MF_ERR_ARG;
-    if (n > ctx->max_n || m > ctx->max_m) return MF_ERR_SHAPE;
-    return MF_OK;
-}
+}  // namespace
 
-int check_predictor(const mf_predictor *p)
+int mf_check_predictor(const mf_predictor *p)
 {
     if (!p || !p->d_W1 || !p->d_b1 || !p->d_W2 || !p->d_b2 || !p->d_W3 || !p->d_b3) return MF_ERR_ARG;
     if (p->F < 1 || p->F > 256 || (p->H != 64 && p->H != 128)) return MF_ERR_ARG;
@@ -31,6 +27,16 @@ int check_predictor(const mf_predictor *p)
     if (p->d_W1sm && (!aligned16(p->d_W1sm) || p->sm_on_feature < 0 || p->sm_on_feature >= p->F ||
                       p->sm_off_feature < 0 || p->sm_off_feature >= p->F))
         return MF_ERR_ARG;
+    if (p->d_ln_w && (!p->d_ln_b || !(p->ln_eps > 0.0f) || isinf(p->ln_eps))) return MF_ERR_ARG;
+    return MF_OK;
+}
+
+namespace {
+
+int check_matrix(const mf_ctx *ctx, const void *d_W, int n, int m, int64_t ldw)
+{
+    if (!ctx || !d_W || n <= 0 || m <= 0 || ldw < m || (ldw & 3) || !aligned16(d_W)) return MF_ERR_ARG;
+    if (n > ctx->max_n || m > ctx->max_m) return MF_ERR_SHAPE;
     return MF_OK;
 }
 
@@ -39,7 +45,7 @@ int check_predictors(const mf_predictor *preds, int n_types)
 {
     if (!preds || n_types < 1 || n_types > MF_MAX_TYPES) return MF_ERR_ARG;
     for (int t = 0; t < n_types; ++t) {
-        const int rc = check_predictor(&preds[t]);
+        const int rc = mf_check_predictor(&preds[t]);
         if (rc != MF_OK) return rc;
         if (preds[t].F != preds[0].F || preds[t].mem_feature != preds[0].mem_feature ||
             preds[t].mem_limit != preds[0].mem_limit || preds[t].scale != preds[0].scale ||
@@ -219,6 +225,7 @@ int mf_create(mf_ctx **out, int device, void *hip_stream, int max_n, int max_m)
     TRY(dev_alloc(&ctx->stats, 1));
     TRY(dev_alloc(&ctx->cert, MF_CERT_PARTS));
     TRY(hipMalloc((void **)&ctx->score_range, 8 * sizeof(unsigned)));
+    TRY(dev_alloc(&ctx->fit_W1, 128 * 512 + 128));
     TRY(hipMalloc((void **)&ctx->score_queue, MF_MAX_TYPES * MF_PAIR_QUEUES * MF_PAIR_QUEUE_STEP * sizeof(int)));
     TRY(hipHostMalloc((void **)&ctx->h_stats, sizeof(mf_device_stats)));
     for (int i = 0; i < 2; ++i) {
@@ -247,7 +254,7 @@ int mf_destroy(mf_ctx *ctx)
     if (!ctx) return MF_ERR_ARG;
     (void)hipSetDevice(ctx->device);
     (void)hipStreamSynchronize(ctx->stream);
-    void *dev[] = {ctx->score_range, ctx->score_queue, ctx->proj_on, ctx->proj_off, ctx->mem_on, ctx->mem_off, ctx->sm_on, ctx->sm_off, ctx->order_on, ctx->order_off, ctx->rank_off, ctx->rank_on, ctx->mem_on_sorted, ctx->mem_off_sorted, ctx->fit_len_on, ctx->fit_len_off, ctx->staged, ctx->type_segment, ctx->pairs_evaluated, ctx->feasible_pairs, ctx->largest_weight, ctx->wt, ctx->price,
+    void *dev[] = {ctx->fit_W1, ctx->score_range, ctx->score_queue, ctx->proj_on, ctx->proj_off, ctx->mem_on, ctx->mem_off, ctx->sm_on, ctx->sm_off, ctx->order_on, ctx->order_off, ctx->rank_off, ctx->rank_on, ctx->mem_on_sorted, ctx->mem_off_sorted, ctx->fit_len_on, ctx->fit_len_off, ctx->staged, ctx->type_segment, ctx->pairs_evaluated, ctx->feasible_pairs, ctx->largest_weight, ctx->wt, ctx->price,
                    ctx->profit, ctx->colword, ctx->roword, ctx->row2col, ctx->col2row, ctx->team_ctl, ctx->path_ctl, ctx->path_label, ctx->path_expanded, ctx->path_frontier[0], ctx->path_frontier[1], ctx->path_stamp, ctx->path_held, ctx->path_base, ctx->path_tree, ctx->path_parent, ctx->path_jump, ctx->edge_count, ctx->edge_start, ctx->list[0], ctx->list[1], ctx->colmark, ctx->stats,
                    ctx->core_entries[0], ctx->core_entries[1], ctx->core_bound[0], ctx->core_bound[1], ctx->core_half_bound[0], ctx->core_half_bound[1], ctx->core_built[0], ctx->core_built[1], ctx->core_reach[0], ctx->core_reach[1],
                    ctx->core_t_entries[0], ctx->core_t_entries[1], ctx->core_t_start[0], ctx->core_t_start[1], ctx->core_t_at[0], ctx->core_t_at[1],
@@ -275,7 +282,7 @@ int mf_score_pairs(mf_ctx *ctx, const mf_predictor *pred, const float *d_on, int
                    const float *d_off, int m, int32_t *d_W, int64_t ldw, float *d_sigma)
 {
     if (!ctx || !d_on || !d_off || !d_W || n <= 0 || m <= 0 || ldw < m) return MF_ERR_ARG;
-    int rc = check_predictor(pred);
+    int rc = mf_check_predictor(pred);
     if (rc != MF_OK) return rc;
     if (n > ctx->max_n || m > ctx->max_m) return MF_ERR_SHAPE;
     MF_HIP(hipSetDevice(ctx->device));
@@ -322,7 +329,7 @@ int mf_schedule_round(mf_ctx *ctx, const mf_predictor *pred, const float *d_on, 
     if (!d_on || !d_off || !d_row2col || !d_u || !d_v || !h_res) return MF_ERR_ARG;
     int rc = check_matrix(ctx, d_W, n, m, ldw);
     if (rc != MF_OK) return rc;
-    rc = check_predictor(pred);
+    rc = mf_check_predictor(pred);
     if (rc != MF_OK) return rc;
     MF_HIP(hipSetDevice(ctx->device));
     clear_timings(ctx);
@@ -385,7 +392,7 @@ int mf_schedule_round_update(mf_ctx *ctx, const mf_predictor *pred, const float 
         return MF_ERR_ARG;
     int rc = check_matrix(ctx, d_W, n, m, ldw);
     if (rc != MF_OK) return rc;
-    rc = check_predictor(pred);
+    rc = mf_check_predictor(pred);
     if (rc != MF_OK) return rc;
     if (n_changed_on > n || n_changed_off > m) return MF_ERR_SHAPE;
     MF_HIP(hipSetDevice(ctx->device));

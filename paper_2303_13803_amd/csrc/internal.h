@@ -234,6 +234,7 @@ struct mf_ctx : mf_options {
     int *score_queue;                   // device: next tasks of the pair kernel's launches, one a type, MF_PAIR_QUEUES counters each
     unsigned *score_range;              // device: largest magnitudes the scorer's fp16 pieces are scaled by (project_kernel)
     mf_cert_out *h_cert;
+    float *fit_W1;                      // device: [128][512] layer 1 with the norm folded in, and [128] its bias (fit.hip)
     // timing
     unsigned long long *times, *h_times;        // [AT_COUNT] device, pinned
     double clock_khz;               // of the clock they are in
@@ -268,6 +269,11 @@ struct SideArgs {
 
 inline long long mf_tail_steps(const mf_ctx *ctx, int side, int lines) { return steps_of_side(side, ctx->phase_tail_sides, ctx->phase_tail_steps, ctx->phase_tail_from, lines); }
 
+// api.hip
+int mf_check_predictor(const mf_predictor *p);
+// layers.hip
+struct DropRule;
+bool mf_drop_rule(const mf_dropout_rule *given, DropRule *rule);        // false: not a valid one
 // report.hip
 int mf_send(mf_ctx *ctx, const mf_report &r, unsigned *number);         // on the stream; *number says which it is
 int mf_await(mf_ctx *ctx, unsigned number);                             // until that one is there

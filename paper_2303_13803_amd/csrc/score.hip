@@ -12,6 +12,7 @@
 // logistic, quantisation and memory-fit mask run in registers before one
 // coalesced int32 store.
 #include "report.h"
+#include "row_sums.h"
 #include <limits.h>
 #include <math.h>
 #include <type_traits>
@@ -42,6 +43,8 @@ struct ProjectArgs {
     float *P[2];
     const float *W1, *b1;
     int F, H;
+    const float *ln_w, *ln_b;                              // of the norm of the features, [2F] (null: none)
+    float ln_eps;
     const float *range_of[3];                              // W2, W1sm, sm_off (the latter two may be null)
     int range_count[3];
     unsigned *range;                                       // null: not wanted
@@ -66,6 +69,7 @@ __global__ __launch_bounds__(256) void project_kernel(ProjectArgs a)
     __shared__ float w_lds[PROJECT_FEATURES][64];
     __shared__ float x_lds[PROJECT_ROWS][PROJECT_FEATURES];
     __shared__ float wave_mx[4];
+    __shared__ float2 moments[PROJECT_ROWS];                // mean and inverse deviation of a workload's features
     const int tiles_on = (a.rows[0] + PROJECT_ROWS - 1) / PROJECT_ROWS, tiles_off = (a.rows[1] + PROJECT_ROWS - 1) / PROJECT_ROWS;
     int tile = blockIdx.x;
     if (tile >= tiles_on + tiles_off) {
@@ -85,6 +89,18 @@ __global__ __launch_bounds__(256) void project_kernel(ProjectArgs a)
     constexpr int MINE = PROJECT_ROWS / 4;
     const int row0 = tile * PROJECT_ROWS, rows = min(PROJECT_ROWS, a.rows[side] - row0);
     const float *X = a.X[side] + (size_t)row0 * a.F, *W = a.W1 + (size_t)k0 * 2 * a.F + (side ? a.F : 0);
+    if (a.ln_w) {                                           // eight lanes a row: the features are in a cache from here on
+        const int r = threadIdx.x / 8, sub = threadIdx.x % 8;
+        if (r < rows) {
+            const float *x = X + (size_t)r * a.F;
+            float s = 0.0f, squares = 0.0f;
+            for (int t = sub; t < a.F; t += 8) s += x[t];
+            const float mean = group_sum<8>(s) / (float)a.F;
+            for (int t = sub; t < a.F; t += 8) { const float d = x[t] - mean; squares = fmaf(d, d, squares); }
+            const float rstd = 1.0f / sqrtf(group_sum<8>(squares) / (float)a.F + a.ln_eps);
+            if (sub == 0) moments[r] = make_float2(mean, rstd);
+        }
+    }
     float sum[MINE];
 #pragma unroll
     for (int r = 0; r < MINE; ++r) sum[r] = side == 0 ? a.b1[k0 + lane] : 0.0f;
@@ -97,7 +113,14 @@ __global__ __launch_bounds__(256) void project_kernel(ProjectArgs a)
         }
         for (int e = threadIdx.x; e < PROJECT_ROWS * PROJECT_FEATURES; e += 256) {
             const int r = e / PROJECT_FEATURES, t = e % PROJECT_FEATURES;
-            if (t < depth) x_lds[r][t] = r < rows ? X[(size_t)r * a.F + t0 + t] : 0.0f;
+            if (t < depth) {
+                float x = r < rows ? X[(size_t)r * a.F + t0 + t] : 0.0f;
+                if (a.ln_w && r < rows) {
+                    const int f = (side ? a.F : 0) + t0 + t;
+                    x = fmaf((x - moments[r].x) * moments[r].y, a.ln_w[f], a.ln_b[f]);
+                }
+                x_lds[r][t] = x;
+            }
         }
         __syncthreads();
         for (int t = 0; t < depth; ++t) {
@@ -992,6 +1015,7 @@ void launch_projections(mf_ctx *ctx, const mf_predictor *p, const float *d_on, i
     a.P[0] = ctx->proj_on; a.P[1] = ctx->proj_off;
     a.W1 = p->d_W1; a.b1 = p->d_b1;
     a.F = p->F; a.H = p->H;
+    a.ln_w = p->d_ln_w; a.ln_b = p->d_ln_b; a.ln_eps = p->ln_eps;
     a.range_of[0] = p->d_W2; a.range_count[0] = p->H * p->H;
     a.range_of[1] = p->d_W1sm; a.range_count[1] = p->H;
     a.range_of[2] = p->d_W1sm ? ctx->sm_off : nullptr; a.range_count[2] = m;
