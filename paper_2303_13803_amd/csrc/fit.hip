@@ -4,372 +4,633 @@
 // For a sample s = (i, j, t), with u the features of both workloads, normalised where the predictor has a layer norm:
 //     x = g u + beta,  z1 = W1 x + b1 (+ share W1sm),  d1 = drop(relu(z1)),  z2 = W2 d1 + b2,  d2 = drop(relu(z2)),
 //     y = logistic(W3 d2 + b3),  loss = scale sum (y - t)^2  (and the same of the slowdown unit),
-//     dz3 = 2 scale (y - t) y (1 - y),  dz2 = [d2 > 0] c W3 dz3,  dz1 = [d1 > 0] c W2^T dz2,
-//     dW2 = sum dz2 d1^T,  G = sum dz1 u^T,  h = sum dz1.
+//     dz3 = 2 (y - t) y (1 - y),  dz2 = [d2 > 0] c W3 dz3,  dz1 = [d1 > 0] c W2^T dz2,
+//     dW2 = sum dz2 d1^T,  G = sum dz1 u^T,  h = sum dz1, and all of that times scale at the end.
 // The norm's weight and bias fold into layer 1, and their gradients come out of sums that layer 1's needs anyway:
 //     W1 x + b1 = (W1 diag g) u + (b1 + W1 beta),  dW1 = G diag g + h beta^T,  dg_f = sum_k W1[k,f] G[k,f],  dbeta = W1^T h,
-// so a sample costs no more than without it.
+// so a sample costs no more than without it.  Nothing of a sample goes to memory but what it predicts.
 //
-// A workgroup takes FIT_ROWS samples at a time through all of that; activations pass from wavefront to wavefront through LDS and
-// gradients of weights stay in the accumulators of its matrix instructions until it has no more samples.  Nothing of a
-// sample goes to memory but what it predicts.  Workgroups' sums are added up by fit_sum_kernel, always in the same order.
-#include "internal.h"
-#include "philox.h"
-#include "row_sums.h"
-#include <math.h>
+// Matrix products.  A float32 operand goes to the fp16 matrix pipe as two fp16 pieces, v = hi + lo with either rounded to nearest
+// (|v - hi - lo| <= 2^-22 |v|), and a product is hi hi + hi lo + lo hi, added up in float32: three fp16 products at sixteen times
+// the rate of the float32 ones (2300 and 152 TFLOP/s measured).  fp16's range is seen to by scaling each operand with a power of two
+// from a bound on it that is never exceeded, to below 2^14; what is within 2^-17 of the bound keeps all its 22 bits, smaller
+// values lose absolute precision of 2^-39 of the bound.  The bounds: a normalised row has |u|_2 <= sqrt(F), so |z1_k| <= |W1_k|_2
+// sqrt(2F) + |b1_k|; |dz3| <= (1 + max |t|) / 2; and through W3 and W2 by their largest values and columns' sums.  Rows of weights have a scale
+// each, of their own largest value.
+//
+// A workgroup takes FIT_ROWS samples at a time.  Half of its wavefronts ("forward", 32 hidden units each) take them through the layers and back;
+// activations pass between them through LDS.  The others ("sums") add up the gradients of weights, in accumulators that stay until there are no
+// more samples, and get the next samples ready: features, their norm, random bits.  A SIMD has one wavefront of either kind, so that the matrix
+// instructions of one run beside the arithmetic of the other:
+//     forward   layer 1 -> d1      layer 2 -> output      loss, dz2           W2^T dz2 -> dz1
+//     sums      G of the last      next features          next random bits    dW2
+//
+// NaN: a ReLU that is one instruction turns it into 0, so what is not finite among the weights, or a sample's features, is added to the output as a NaN.
+#include "fit_parts.h"
 
-typedef float floatx16 __attribute__((ext_vector_type(16)));
+typedef _Float16 half2v __attribute__((ext_vector_type(2)));
+typedef _Float16 half4v __attribute__((ext_vector_type(4)));
+typedef _Float16 half8v __attribute__((ext_vector_type(8)));
+typedef float float2v __attribute__((ext_vector_type(2)));
+typedef short short4v __attribute__((ext_vector_type(4)));
 
 namespace {
 
-constexpr int FIT_ROWS = 64, FIT_CHUNK = 64;                // samples a workgroup takes at a time; features staged at a time
-constexpr int FIT_COLUMNS_MAX = 512;                        // 2F, at most
-constexpr int FIT_PASS_TILES = 8;                           // column tiles of G that one pass over the samples can keep
+constexpr int FIT_ROWS = 32;
 
-struct FitArgs {
-    const float *X[2];
-    int rows[2], F, columns, padded;                        // columns = 2F, padded to a multiple of 32
-    const int32_t *index[2];
-    const float *target[2];                                 // throughput, slowdown (null: not trained)
-    float *sigma[2];                                        // (null: not wanted)
-    long long count;
-    const float *W1, *b1;                                   // folded, [H][padded] and [H]
-    const float *W2, *b2, *W3[2], *b3[2], *W1sm;            // ([1] and W1sm may be null)
-    int norm, sm_feature[2];
-    float eps, scale;
-    int drop;
-    DropRule rule;
-    const unsigned long long *step;
-    float *partial;
-    long long partial_step;
-};
-
-// What a workgroup leaves, one after the other.
-template <int H>
-struct FitSums {
-    static constexpr int W2 = 0, B1 = H * H, B2 = B1 + H, W3 = B2 + H, W3S = W3 + H, SM = W3S + H, REST = SM + H, G = REST + 4;
-};
-enum { REST_B3 = 0, REST_B3S, REST_LOSS };
-
-// Row r of a 32-row tile of matrix results lies in lane half (r >> 2) & 1; read as unit tile_unit(r), what a lane holds of
-// a tile are the units 8 half .. 8 half + 7 and 16 + 8 half .. 16 + 8 half + 7: eight that share a counter.
-__device__ __forceinline__ int tile_unit(int r) { return (r & 0x13) | (r & 4) << 1 | (r & 8) >> 1; }
-
-__device__ __forceinline__ float other_half(float v)
+// The largest power of two that takes a value of at most `bound` to below 2^14 (1 for bounds that are none).
+__device__ __forceinline__ float scale_below(float bound)
 {
-    const auto s = __builtin_amdgcn_permlane32_swap(__float_as_uint(v), __float_as_uint(v), false, false);
-    return __uint_as_float(s[0]) + __uint_as_float(s[1]);
+    if (!(bound > 0.0f) || bound > 1e30f) return 1.0f;
+    int e;
+    (void)frexpf(bound, &e);                                // bound < 2^e
+    e = e < -96 ? -96 : e > 96 ? 96 : e;
+    return ldexpf(1.0f, 14 - e);
 }
 
-// max(v, 0) that keeps a NaN: a fit that has diverged shows.
-__device__ __forceinline__ float relu(float v) { return v < 0.0f ? 0.0f : v; }
-
-template <int H>
-constexpr size_t fit_lds_bytes(bool grad)
+// v = hi + lo in fp16, to 22 bits.  The remainder is exact; written as a fused multiply-add by a -1 that the optimiser cannot see it is one
+// instruction that reads the fp16 piece itself.
+template <int N>
+__device__ __forceinline__ void split(const float (&v)[N], _Float16 (&hi)[N], _Float16 (&lo)[N], const float minus_one)
 {
-    return sizeof(float) * ((size_t)H * (H + 4) + FIT_ROWS * (FIT_CHUNK + 4) + (size_t)FIT_ROWS * (H + 4) * (grad ? 2 : 1) +
-                            2 * (H / 32) * FIT_ROWS + FIT_ROWS * 5 + 4 * FIT_ROWS + 5 * H);
-}
-
-template <int H, int GT, bool GRAD>
-__global__ __launch_bounds__(H * 4) void fit_kernel(FitArgs a)
-{
-    constexpr int T = FIT_ROWS, PITCH = H + 4, XP = FIT_CHUNK + 4, UB = H / 32, THREADS = H * 4, QUADS = H / 8;
-    using S = FitSums<H>;
-    extern __shared__ __align__(16) float lds[];
-    float *w2 = lds, *xs = w2 + H * PITCH, *act = xs + T * XP, *back = act + T * PITCH;
-    float *part = back + (GRAD ? T * PITCH : 0), *target = part + 2 * UB * T, *target_slow = target + T, *share = target_slow + T;
-    int *at_on = (int *)(share + T), *at_off = at_on + T;
-    float2 *moments = (float2 *)(at_off + T);
-    float *vec = (float *)(moments + 2 * T);                // b1, b2, W3, W3 of the slowdown unit, W1sm
-    const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6, nn = lane & 31, hh = lane >> 5;
-    const int ub = wave % UB, sh = wave / UB;               // units 32 ub .. and samples 32 sh .. of the forward pass are this wavefront's
-    const int unit = 32 * ub + tile_unit(nn), mine = 32 * sh + nn, u0 = 32 * ub + 8 * hh;
-    if (a.step) { const unsigned long long s = *a.step; a.rule.s0 = (unsigned)s; a.rule.s1 = (unsigned)(s >> 32); }
-
-    for (int e = tid; e < H * H / 4; e += THREADS) *(float4 *)(w2 + e / (H / 4) * PITCH + e % (H / 4) * 4) = ((const float4 *)a.W2)[e];
-    for (int e = tid; e < H; e += THREADS) {
-        vec[e] = a.b1[e];
-        vec[H + e] = a.b2[e];
-        vec[2 * H + e] = a.W3[0][e];
-        vec[3 * H + e] = a.W3[1] ? a.W3[1][e] : 0.0f;
-        vec[4 * H + e] = a.W1sm ? a.W1sm[e] : 0.0f;
+#pragma unroll
+    for (int t = 0; t < N; t += 2) {
+        const float2v x = {v[t], v[t + 1]};
+        const half2v h = __builtin_convertvector(x, half2v);
+        const float2v r = {__builtin_fmaf((float)h[0], minus_one, v[t]), __builtin_fmaf((float)h[1], minus_one, v[t + 1])};
+        const half2v l = __builtin_convertvector(r, half2v);
+        hi[t] = h[0]; hi[t + 1] = h[1];
+        lo[t] = l[0]; lo[t + 1] = l[1];
     }
-    const float b3 = *a.b3[0], b3s = a.W3[1] ? *a.b3[1] : 0.0f;
-    const float factor = a.drop ? a.rule.factor : 1.0f;
-    const int chunks = (a.padded + FIT_CHUNK - 1) / FIT_CHUNK;
-    const int pass_chunk = blockIdx.y * (FIT_PASS_TILES / 2);       // this pass keeps G from this chunk on
+}
+__device__ __forceinline__ float hidden_minus_one()
+{
+    float v = -1.0f;
+    asm volatile("" : "+s"(v));                             // no instruction
+    return v;
+}
 
-    floatx16 gw2[UB / 2], gw1[GT];
-    float gb1[16], gb2[16], gw3[16], gw3s[16], gsm[16], gb3 = 0.0f, gb3s = 0.0f, loss = 0.0f;
+struct Frag { half8v hi, lo; };
+
+__device__ __forceinline__ floatx16 product(const Frag &a, const Frag &b, floatx16 c)
+{
+    c = __builtin_amdgcn_mfma_f32_32x32x16_f16(a.hi, b.hi, c, 0, 0, 0);
+    c = __builtin_amdgcn_mfma_f32_32x32x16_f16(a.hi, b.lo, c, 0, 0, 0);
+    return __builtin_amdgcn_mfma_f32_32x32x16_f16(a.lo, b.hi, c, 0, 0, 0);
+}
+
+// Eight values of a matrix kept in rows [sample][column], for sums over samples: lane l gets column `first` + l % 32 of samples
+// 8 (l / 32) .. + 7.  The transposing read gives a group of sixteen lanes four rows of sixteen columns, a column to each lane.
+__device__ __forceinline__ half8v read_columns(const _Float16 *m, int pitch, int first, int lane)
+{
+    const int group = lane >> 4, i = lane & 15;
+    const _Float16 *p = m + (8 * (group >> 1) + (i >> 2)) * pitch + first + 16 * (group & 1) + 4 * (i & 3);
+    const auto read = [](const _Float16 *q) {
+        return __builtin_bit_cast(half4v, __builtin_amdgcn_ds_read_tr16_b64_v4i16((__attribute__((address_space(3))) short4v *)q));
+    };
+    const half4v a = read(p), b = read(p + 4 * pitch);
+    return __builtin_shufflevector(a, b, 0, 1, 2, 3, 4, 5, 6, 7);
+}
+
+__device__ __forceinline__ float wave_max(float v)
+{
+#pragma unroll
+    for (int off = 32; off >= 1; off >>= 1) v = fmaxf(v, __shfl_xor(v, off));
+    return v;
+}
+
+// Waits for what this wavefront has put into or read from LDS, and for the other wavefronts to have come here, but not for loads and stores of
+// global memory on their way: features are fetched a stage before they are looked at.
+__device__ __forceinline__ void meet()
+{
+    __builtin_amdgcn_fence(__ATOMIC_RELEASE, "workgroup", "local");
+    __builtin_amdgcn_s_barrier();
+    __builtin_amdgcn_fence(__ATOMIC_ACQUIRE, "workgroup", "local");
+}
+
+// Everything of a workgroup's that wavefronts share.  Rows of pieces are 16 halves longer than what they hold: eight words, so that
+// eight rows next to each other lie in different banks.
+template <int H, int CT, bool GRAD>
+struct FitShared {
+    static constexpr int T = FIT_ROWS, UB = H / 32, KB = H / 16, HP = H + 16, XP = 32 * CT + 16;
+    half8v w2t[GRAD ? UB : 1][GRAD ? KB : 1][2][64];        // W2^T as operands: [units of layer 1][of layer 2][piece][lane]
+    _Float16 d1[2][T][HP];                                  // [piece]
+    _Float16 xs[2][2][T][XP];                               // [of which samples][piece]
+    _Float16 dz2[GRAD ? 2 : 1][GRAD ? T : 1][HP], dz1[GRAD ? 2 : 1][GRAD ? T : 1][HP];
+    float part[2][UB][T];                                   // output units: partial sums over 32 hidden units
+    float target[2][2][T], share[2][T], bad[2][2][T];       // bad: NaN where features are not finite
+    int real[2][T];
+    unsigned char keep[2][T][H / 8];                        // [layer]: which of eight units stay
+    float b1[H], wsm[H], b2[H], w3[2][H];                   // by unit; b1, wsm and b2 with the scale and the dropout's factor of their layer
+    float most[5][2 * UB];
+};
+
+// Layer 1 with the norm's weight and bias folded in, for the forward wavefronts' operands (or, wide, as rows of floats), with what its
+// bounds are made of; the last FIT_RANGE_PARTS workgroups find the largest target and, where nothing else bounds them, feature.
+struct FoldArgs {
+    const float *W1, *b1, *g, *beta;
+    int H, F, padded, half, wide;
+    void *image;                                            // wide: [H][padded] floats; else fragments of pieces
+    float *bias, *norm1, *norm2, *scale;                    // [H]; [1]
+    float *ranges;                                          // [2][FIT_RANGE_PARTS]: targets, features
+    const float *target[2], *X[2];
+    const int32_t *index[2];
+    int rows[2], features;                                  // features: 0 not wanted, 1 of all workloads, 2 of those the samples name
+    long long count;
+};
+
+__global__ __launch_bounds__(256) void fold_kernel(FoldArgs a)
+{
+    const int lane = threadIdx.x & 63, rows = a.H / 4;
+    if ((int)blockIdx.x >= rows) {
+        __shared__ float most[2][4];
+        const int part = blockIdx.x - rows;
+        const long long first = (long long)part * 256 + threadIdx.x, step = FIT_RANGE_PARTS * 256;
+        float t = 0.0f, x = 0.0f;
+        for (int k = 0; k < 2; ++k)
+            if (a.target[k])
+                for (long long s = first; s < a.count; s += step) { const float v = fabsf(a.target[k][s]); if (v < INFINITY) t = fmaxf(t, v); }
+        for (int k = 0; k < 2; ++k) {
+            if (a.features == 1)
+                for (long long e = first; e < (long long)a.rows[k] * a.F; e += step) { const float v = fabsf(a.X[k][e]); if (v < INFINITY) x = fmaxf(x, v); }
+            if (a.features == 2)
+                for (long long s = first; s < a.count; s += step) {
+                    const int i = a.index[k][s];
+                    if (i < 0 || i >= a.rows[k]) continue;
+                    for (int f = 0; f < a.F; ++f) { const float v = fabsf(a.X[k][(size_t)i * a.F + f]); if (v < INFINITY) x = fmaxf(x, v); }
+                }
+        }
+        t = wave_max(t);
+        x = wave_max(x);
+        if (lane == 0) { most[0][threadIdx.x >> 6] = t; most[1][threadIdx.x >> 6] = x; }
+        __syncthreads();
+        if (threadIdx.x < 2) a.ranges[threadIdx.x * FIT_RANGE_PARTS + part] = fmaxf(fmaxf(most[threadIdx.x][0], most[threadIdx.x][1]), fmaxf(most[threadIdx.x][2], most[threadIdx.x][3]));
+        return;
+    }
+    const auto folded = [&](const int k, const int c, float *times_beta) {
+        const int side = c >= a.half, f = c - side * a.half;
+        if (f >= a.F) return 0.0f;
+        const int at = side * a.F + f;
+        const float w = a.W1[(size_t)k * 2 * a.F + at];
+        if (times_beta) *times_beta = a.g ? w * a.beta[at] : 0.0f;
+        return a.g ? w * a.g[at] : w;
+    };
+    const int k = blockIdx.x * 4 + (threadIdx.x >> 6);
+    float sum = 0.0f, norm1 = 0.0f, norm2 = 0.0f;
+    for (int c = lane; c < a.padded; c += 64) {
+        float more = 0.0f;
+        const float v = folded(k, c, &more);
+        sum += more;
+        norm1 += fabsf(v);
+        norm2 = fmaf(v, v, norm2);
+        if (a.wide) ((float *)a.image)[(size_t)k * a.padded + c] = v;
+    }
+    sum = group_sum<64>(sum);
+    norm1 = group_sum<64>(norm1);
+    norm2 = group_sum<64>(norm2);
+    if (lane == 0) {
+        a.bias[k] = a.b1[k] + sum;
+        a.norm1[k] = norm1;
+        a.norm2[k] = sqrtf(norm2);
+    }
+    if (a.wide) return;
+    // (every workgroup looks for the largest weight itself: no more than 48 KB, and no launch between)
+    __shared__ float most[4];
+    float largest = 0.0f;
+#pragma unroll 8
+    for (int e = threadIdx.x; e < a.H * 2 * a.F; e += 256) largest = fmaxf(largest, fabsf(a.g ? a.W1[e] * a.g[e % (2 * a.F)] : a.W1[e]));
+    largest = wave_max(largest);
+    if (lane == 0) most[threadIdx.x >> 6] = largest;
+    __syncthreads();
+    const float scale = scale_below(fmaxf(fmaxf(most[0], most[1]), fmaxf(most[2], most[3])));
+    if (blockIdx.x == 0 && threadIdx.x == 0) *a.scale = scale;
+    const int blocks = a.padded / 16, m = tile_unit(k & 31);
+    for (int c = lane; c < a.padded; c += 64) {
+        const float v[2] = {folded(k, c, nullptr) * scale, 0.0f};
+        _Float16 hi[2], lo[2];
+        split(v, hi, lo, -1.0f);
+        _Float16 *to = (_Float16 *)a.image + ((size_t)((k >> 5) * blocks + (c >> 4)) * 2 * 64 + ((c >> 3) & 1) * 32 + m) * 8 + (c & 7);
+        to[0] = hi[0];
+        to[64 * 8] = lo[0];
+    }
+}
+
+// EXTRA: the predictor has the slowdown unit or the SM share (or both).
+template <int H, int CT, bool GRAD, bool EXTRA>
+__global__ __launch_bounds__(H * 4, 2) void fit_kernel(FitArgs a, const float *__restrict__ scale1, const float *__restrict__ norm1, const float *__restrict__ norm2,
+                                                       const float *__restrict__ ranges)
+{
+    using L = FitShared<H, CT, GRAD>;
+    using S = FitSums<H>;
+    constexpr int T = FIT_ROWS, UB = H / 32, KB = H / 16, XB = 2 * CT, HALF = 16 * CT, HP = L::HP, XP = L::XP;
+    extern __shared__ __align__(16) char lds[];
+    L &sh = *(L *)lds;
+    const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), nn = lane & 31, hh = lane >> 5;
+    const float minus_one = hidden_minus_one();
+    if (a.step) { const unsigned long long s = *a.step; a.rule.s0 = (unsigned)s; a.rule.s1 = (unsigned)(s >> 32); }
+    const bool slow = EXTRA && a.W3[1], with_share = EXTRA && a.W1sm;
+    const float factor = a.drop ? a.rule.factor : 1.0f;
+    const long long tiles = (a.count + T - 1) / T;
+    const int mine = (int)((tiles - blockIdx.x + gridDim.x - 1) / gridDim.x);
+    const auto tile_of = [&](const int it) { return (long long)blockIdx.x + (long long)it * gridDim.x; };
+    const bool forward = wave < UB;
+    const int ub = forward ? wave : wave - UB, unit = 32 * ub + tile_unit(nn), u0 = 32 * ub + 8 * hh;
+
+    // ---- bounds, and the scales that follow.  W2 and its transpose are read as the operands that the forward wavefronts make of them.
+    float w[KB][8], largest = 0.0f, column = 0.0f, poison = 0.0f;
+    if (forward) {
+#pragma unroll
+        for (int b = 0; b < KB; ++b)
+#pragma unroll
+            for (int e = 0; e < 8; ++e) {
+                w[b][e] = a.W2[(16 * b + 8 * hh + e) * H + unit];
+                largest = fmaxf(largest, fabsf(w[b][e]));
+                column += fabsf(w[b][e]);
+            }
+        column = both_halves(column);
+        poison = column * 0.0f;                             // NaN if one of them is not finite
+    }
+    // largest of: targets, features, output weights of either unit, W2 and its columns' sums, z1
+    float v[6] = {0.0f, 0.0f, 0.0f, 0.0f, largest, column};
+    if (tid < FIT_RANGE_PARTS) { v[0] = ranges[tid]; v[1] = ranges[FIT_RANGE_PARTS + tid]; }
+    if (tid < H) {
+        v[2] = fabsf(a.W3[0][tid]);
+        v[3] = slow ? fabsf(a.W3[1][tid]) : 0.0f;
+        poison += (norm1[tid] + a.b1[tid] + a.b2[tid] + (with_share ? a.W1sm[tid] : 0.0f)) * 0.0f;
+    }
+    const auto most_of = [&](float (&v)[6]) {
+#pragma unroll
+        for (int q = 0; q < 6; ++q) v[q] = wave_max(v[q]);
+        for (int q = 0; q < 6; q += 5) {                    // five at a time
+            __syncthreads();
+#pragma unroll
+            for (int k = 0; k < 5; ++k) if (q + k < 6 && lane == 0) sh.most[k][wave] = v[q + k];
+            __syncthreads();
+#pragma unroll
+            for (int k = 0; k < 5; ++k)
+                if (q + k < 6)
+                    for (int x = 0; x < 2 * UB; ++x) v[q + k] = fmaxf(v[q + k], sh.most[k][x]);
+        }
+    };
+    most_of(v);
+    const float most_x = v[1], length = sqrtf((float)a.F);
+    const float s_x = scale_below(a.norm ? length * 1.001f : most_x), s_w2 = scale_below(v[4]);
+    const float bound2 = 0.5f * (1.0f + v[0]) * (v[2] + v[3]) * factor * 1.001f;
+    const float s_dz2 = scale_below(bound2), s_dz1 = scale_below(bound2 * factor * v[5] * 1.001f);
+    float z1 = 0.0f;
+    if (tid < H) {
+        z1 = fabsf(a.b1[tid]) + (a.norm ? norm2[tid] * length * 1.42f : norm1[tid] * most_x);
+        if (with_share) z1 += fabsf(a.W1sm[tid]) * (1.0f + most_x);
+    }
+    z1 = wave_max(z1);
+    poison = group_sum<64>(poison);
+    __syncthreads();
+    if (lane == 0) { sh.most[0][wave] = z1; sh.most[1][wave] = poison; }
+    __syncthreads();
+    poison = 0.0f;
+    for (int x = 0; x < 2 * UB; ++x) { z1 = fmaxf(z1, sh.most[0][x]); poison += sh.most[1][x]; }
+    const float s_d1 = scale_below(z1 * factor * 1.001f);
+    // what accumulators of the three products are multiplied with
+    const float by_z1 = factor * s_d1 / (s_x * *scale1), by_z2 = factor / (s_d1 * s_w2), by_d1 = factor * s_dz1 / (s_dz2 * s_w2), by_dz = factor * s_dz2;
+    if (tid < H) {
+        sh.b1[tid] = a.b1[tid] * (factor * s_d1);
+        sh.wsm[tid] = with_share ? a.W1sm[tid] * (factor * s_d1) : 0.0f;
+        sh.b2[tid] = a.b2[tid] * factor;
+        sh.w3[0][tid] = a.W3[0][tid];
+        sh.w3[1][tid] = slow ? a.W3[1][tid] : 0.0f;
+    }
+    const auto as_operand = [&](const float (&from)[8]) {
+        float v[8];
+        _Float16 hi[8], lo[8];
+#pragma unroll
+        for (int e = 0; e < 8; ++e) v[e] = from[e] * s_w2;
+        split(v, hi, lo, minus_one);
+        Frag f;
+#pragma unroll
+        for (int e = 0; e < 8; ++e) { f.hi[e] = hi[e]; f.lo[e] = lo[e]; }
+        return f;
+    };
+    float *out = a.partial ? a.partial + (size_t)blockIdx.x * a.partial_step : nullptr;
+
+    if (forward) {
+        if (GRAD) {
+#pragma unroll
+            for (int b = 0; b < KB; ++b) {
+                const Frag f = as_operand(w[b]);
+                sh.w2t[ub][b][0][lane] = f.hi;
+                sh.w2t[ub][b][1][lane] = f.lo;
+            }
+        }
+        Frag w2[KB];
+#pragma unroll
+        for (int b = 0; b < KB; ++b) {
+            float v[8];
+            __builtin_memcpy(v, __builtin_assume_aligned(a.W2 + unit * H + 16 * b + 8 * hh, 16), sizeof(v));
+            w2[b] = as_operand(v);
+        }
+        const float b3[2] = {*a.b3[0] + poison, slow ? *a.b3[1] + poison : 0.0f};
+        float gw3[16], gw3s[16], gb3[2] = {0.0f, 0.0f}, loss = 0.0f;
+#pragma unroll
+        for (int k = 0; k < 16; ++k) gw3[k] = gw3s[k] = 0.0f;
+        const half8v *image = (const half8v *)a.W1 + (size_t)ub * XB * 2 * 64 + lane;
+        // eight values to a sample's row, as pieces
+        const auto put = [&](_Float16 *hi_to, _Float16 *lo_to, const float (&v)[8]) {
+            _Float16 hi[8], lo[8];
+            split(v, hi, lo, minus_one);
+            half8v h, l;
+#pragma unroll
+            for (int e = 0; e < 8; ++e) { h[e] = hi[e]; l[e] = lo[e]; }
+            *(half8v *)hi_to = h;
+            *(half8v *)lo_to = l;
+        };
+        // a unit's value after ReLU and dropout: its bit, as a mask
+        const auto kept = [](const float z, const unsigned keep, const int e) {
+            return __uint_as_float(__float_as_uint(fmaxf(z, 0.0f)) & (unsigned)((int)(keep << (31 - e)) >> 31));
+        };
+        const floatx16 zero = {0};
+        meet();                                             // the first samples are there
+        for (int it = 0; it < mine; ++it) {
+            const int now = it & 1;
+            floatx16 z;
+            bool open1[16];
+#pragma unroll
+            for (int b = 0; b < XB; ++b) {
+                const Frag w = {image[(2 * b) * 64], image[(2 * b + 1) * 64]};
+                const Frag x = {*(const half8v *)&sh.xs[now][0][nn][16 * b + 8 * hh], *(const half8v *)&sh.xs[now][1][nn][16 * b + 8 * hh]};
+                z = product(w, x, b == 0 ? zero : z);
+            }
+            const float share = with_share ? sh.share[now][nn] : 0.0f;
+#pragma unroll
+            for (int g = 0; g < 2; ++g) {
+                const unsigned keep = a.drop ? sh.keep[0][nn][4 * ub + hh + 2 * g] : 255u;
+                float v[8];
+#pragma unroll
+                for (int e = 0; e < 8; ++e) {
+                    const int k = u0 + 16 * g + e;
+                    float h = fmaf(z[8 * g + e], by_z1, sh.b1[k]);
+                    if (EXTRA) h = fmaf(share, sh.wsm[k], h);
+                    v[e] = kept(h, keep, e);
+                    open1[8 * g + e] = v[e] > 0.0f;
+                }
+                put(&sh.d1[0][nn][u0 + 16 * g], &sh.d1[1][nn][u0 + 16 * g], v);
+            }
+            meet();
+#pragma unroll
+            for (int b = 0; b < KB; ++b) {
+                const Frag x = {*(const half8v *)&sh.d1[0][nn][16 * b + 8 * hh], *(const half8v *)&sh.d1[1][nn][16 * b + 8 * hh]};
+                z = product(w2[b], x, b == 0 ? zero : z);
+            }
+            float h2[16], zp = 0.0f, zs = 0.0f;
+#pragma unroll
+            for (int g = 0; g < 2; ++g) {
+                const unsigned keep = a.drop ? sh.keep[1][nn][4 * ub + hh + 2 * g] : 255u;
+#pragma unroll
+                for (int e = 0; e < 8; ++e) {
+                    const int k = u0 + 16 * g + e;
+                    const float h = kept(fmaf(z[8 * g + e], by_z2, sh.b2[k]), keep, e);
+                    h2[8 * g + e] = h;
+                    zp = fmaf(sh.w3[0][k], h, zp);
+                    if (EXTRA) zs = fmaf(sh.w3[1][k], h, zs);
+                }
+            }
+            zp = both_halves(zp);
+            if (EXTRA) zs = both_halves(zs);
+            if (hh == 0) { sh.part[0][ub][nn] = zp; if (EXTRA) sh.part[1][ub][nn] = zs; }
+            meet();
+            const long long sample = tile_of(it) * T + nn;
+            const bool real = sh.real[now][nn], speaks = ub == 0 && hh == 0;
+            const float bad = sh.bad[now][0][nn] + sh.bad[now][1][nn];
+            float dz[2] = {0.0f, 0.0f};
+#pragma unroll
+            for (int q = 0; q < (EXTRA ? 2 : 1); ++q) {
+                if (q == 1 && !slow) break;
+                float zq = b3[q] + bad;
+#pragma unroll
+                for (int k = 0; k < UB; ++k) zq += sh.part[q][k][nn];
+                const float y = 1.0f / (1.0f + expf(-zq));
+                if (speaks && a.sigma[q] && sample < a.count) a.sigma[q][sample] = real ? y : 0.0f;
+                // what nobody has measured (a NaN) has no part in the loss
+                const float t = sh.target[now][q][nn], miss = t == t ? y - t : 0.0f;
+                dz[q] = t == t ? 2.0f * miss * y * (1.0f - y) : 0.0f;
+                if (speaks) { loss = fmaf(miss, miss, loss); gb3[q] += dz[q]; }
+            }
+            if (!GRAD) continue;
+            const float c0 = dz[0] * by_dz, c1 = dz[1] * by_dz;
+#pragma unroll
+            for (int g = 0; g < 2; ++g) {
+                float d[8];
+#pragma unroll
+                for (int e = 0; e < 8; ++e) {
+                    const int r = 8 * g + e, k = u0 + 16 * g + e;
+                    float v = c0 * sh.w3[0][k];
+                    gw3[r] = fmaf(dz[0], h2[r], gw3[r]);
+                    if (EXTRA) {
+                        v = fmaf(c1, sh.w3[1][k], v);
+                        gw3s[r] = fmaf(dz[1], h2[r], gw3s[r]);
+                    }
+                    d[e] = h2[r] > 0.0f ? v : 0.0f;
+                }
+                put(&sh.dz2[0][nn][u0 + 16 * g], &sh.dz2[1][nn][u0 + 16 * g], d);
+            }
+            meet();
+#pragma unroll
+            for (int b = 0; b < KB; ++b) {
+                const Frag w = {sh.w2t[ub][b][0][lane], sh.w2t[ub][b][1][lane]};
+                const Frag x = {*(const half8v *)&sh.dz2[0][nn][16 * b + 8 * hh], *(const half8v *)&sh.dz2[1][nn][16 * b + 8 * hh]};
+                z = product(w, x, b == 0 ? zero : z);
+            }
+#pragma unroll
+            for (int g = 0; g < 2; ++g) {
+                float d[8];
+#pragma unroll
+                for (int e = 0; e < 8; ++e) d[e] = open1[8 * g + e] ? z[8 * g + e] * by_d1 : 0.0f;
+                put(&sh.dz1[0][nn][u0 + 16 * g], &sh.dz1[1][nn][u0 + 16 * g], d);
+            }
+            meet();
+        }
+        if (!out) return;
+        if (GRAD) {
+#pragma unroll
+            for (int k = 0; k < 16; ++k) {
+                const float v = group_sum<32>(gw3[k]), vs = EXTRA ? group_sum<32>(gw3s[k]) : 0.0f;
+                if (nn == 0) { out[S::W3 + u0 + 16 * (k >> 3) + (k & 7)] = v; out[S::W3S + u0 + 16 * (k >> 3) + (k & 7)] = vs; }
+            }
+        }
+        if (ub == 0) {
+            const float v[3] = {group_sum<64>(gb3[0]), group_sum<64>(gb3[1]), group_sum<64>(loss)};
+            if (lane == 0)
+#pragma unroll
+                for (int q = 0; q < 3; ++q) out[S::REST + q] = v[q];
+        }
+        return;
+    }
+
+    // ---- sums, and what is to come.  UB neighbouring lanes take the features of one side of a sample, EACH of them each.
+    constexpr int EACH = HALF / UB;
+    const int place = tid - 64 * UB, row = place / UB, sub = place % UB, own = row >> 1, side = row & 1;
+    float x[EACH], next_target[2] = {0.0f, 0.0f}, next_share = 0.0f;
+    int ahead[2] = {-1, -1};                                // the pair that this lane's sample of the tile after the next names
+    bool next_real = false;
+    const auto look = [&](const int it) {                   // at indices
+        ahead[0] = ahead[1] = -1;
+        const long long s = tile_of(it) * T + own;
+        if (it < mine && s < a.count) { ahead[0] = a.index[0][s]; ahead[1] = a.index[1][s]; }
+    };
+    const auto fetch = [&](const int it) {                  // features and targets of the samples whose indices have been looked at
+        // a sample that names no pair has no part in anything
+        next_real = ahead[0] >= 0 && ahead[0] < a.rows[0] && ahead[1] >= 0 && ahead[1] < a.rows[1];
+        const long long s = tile_of(it) * T + own;
+#pragma unroll
+        for (int e = 0; e < EACH; ++e) x[e] = 0.0f;
+        if (next_real) {
+            const float *from = a.X[side] + (size_t)ahead[side] * a.F + sub * EACH;
+            if ((sub + 1) * EACH <= a.F) {
+                __builtin_memcpy(x, from, sizeof(x));
+            } else {
+#pragma unroll
+                for (int e = 0; e < EACH; ++e) if (sub * EACH + e < a.F) x[e] = from[e];
+            }
+        }
+        if (sub == 0 && side == 0) {
+            const float none = __builtin_nanf("");
+            next_target[0] = next_real && a.target[0] ? a.target[0][s] : none;
+            next_target[1] = next_real && a.target[1] ? a.target[1][s] : none;
+            if (with_share)
+                next_share = next_real ? fminf(1.0f - a.X[0][(size_t)ahead[0] * a.F + a.sm_feature[0]], a.X[1][(size_t)ahead[1] * a.F + a.sm_feature[1]]) : 0.0f;
+        }
+    };
+    const auto stage = [&](const int it) {                  // what has been fetched, normalised, as pieces
+        const int to = it & 1;
+        float sum = 0.0f, mean = 0.0f, by = s_x;
+#pragma unroll
+        for (int e = 0; e < EACH; ++e) sum += x[e];
+        sum = group_sum<UB>(sum);
+        if (a.norm) {
+            float squares = 0.0f;
+            mean = sum / (float)a.F;
+#pragma unroll
+            for (int e = 0; e < EACH; ++e) {
+                const float d = sub * EACH + e < a.F ? x[e] - mean : 0.0f;
+                squares = fmaf(d, d, squares);
+            }
+            by = s_x / sqrtf(group_sum<UB>(squares) / (float)a.F + a.eps);
+        }
+        float v[EACH];
+        _Float16 hi[EACH], lo[EACH];
+#pragma unroll
+        for (int e = 0; e < EACH; ++e) v[e] = sub * EACH + e < a.F && next_real ? (x[e] - mean) * by : 0.0f;
+        split(v, hi, lo, minus_one);
+#pragma unroll
+        for (int e = 0; e < EACH; e += 4) {
+            *(half4v *)&sh.xs[to][0][own][side * HALF + sub * EACH + e] = half4v{hi[e], hi[e + 1], hi[e + 2], hi[e + 3]};
+            *(half4v *)&sh.xs[to][1][own][side * HALF + sub * EACH + e] = half4v{lo[e], lo[e + 1], lo[e + 2], lo[e + 3]};
+        }
+        if (sub == 0) {
+            sh.bad[to][side][own] = next_real ? sum * 0.0f : 0.0f;
+            if (side == 0) {
+                sh.target[to][0][own] = next_target[0];
+                sh.target[to][1][own] = next_target[1];
+                sh.share[to][own] = next_share;
+                sh.real[to][own] = next_real;
+            }
+        }
+    };
+    const auto draw = [&](const int it, const int layer) {  // random bits
+#pragma unroll
+        for (int q = 0; q < T * (H / 8) / (64 * UB); ++q) {
+            const int at = place + q * 64 * UB, s = at / (H / 8), k = at % (H / 8);
+            const Words4 bits = drop_bits(a.rule, (unsigned long long)(tile_of(it) * T + s) * (H / 8) + k, layer);
+            unsigned keep = 0;
+#pragma unroll
+            for (int e = 0; e < 8; ++e) keep |= drop_keeps(a.rule, bits, e) ? 1u << e : 0u;
+            sh.keep[layer][s][k] = (unsigned char)keep;
+        }
+    };
+    look(0);
+    fetch(0);
+    stage(0);
+    look(1);
+    if (a.drop) { draw(0, 0); draw(0, 1); }
+    floatx16 gw2[GRAD ? UB : 1], gw1[GRAD ? CT : 1];
+    float gb1 = 0.0f, gb2 = 0.0f, gsm = 0.0f, one = 1.0f;
+    asm volatile("" : "+s"(one));                           // no instruction (see split)
     if (GRAD) {
 #pragma unroll
         for (int e = 0; e < 16; ++e) {
-            gb1[e] = gb2[e] = gw3[e] = gw3s[e] = gsm[e] = 0.0f;
 #pragma unroll
-            for (int t = 0; t < UB / 2; ++t) gw2[t][e] = 0.0f;
+            for (int t = 0; t < UB; ++t) gw2[t][e] = 0.0f;
 #pragma unroll
-            for (int t = 0; t < GT; ++t) gw1[t][e] = 0.0f;
+            for (int t = 0; t < CT; ++t) gw1[t][e] = 0.0f;
         }
     }
-    // features of columns 64 chunk .. 64 chunk + 63
-    auto stage = [&](const int chunk) {
-        for (int e = tid; e < T * FIT_CHUNK; e += THREADS) {
-            const int s = e / FIT_CHUNK, c = chunk * FIT_CHUNK + e % FIT_CHUNK, side = c >= a.F;
-            float v = 0.0f;
-            if (c < a.columns && at_on[s] >= 0) {
-                const float2 m = moments[2 * s + side];
-                v = (a.X[side][(size_t)(side ? at_off[s] : at_on[s]) * a.F + c - (side ? a.F : 0)] - m.x) * m.y;
-            }
-            xs[s * XP + e % FIT_CHUNK] = v;
+    const auto columns_of = [&](const _Float16 *hi, const _Float16 *lo, const int pitch, const int first) {
+        return Frag{read_columns(hi, pitch, first, lane), read_columns(lo, pitch, first, lane)};
+    };
+    const auto add_w1 = [&](const int of) {
+#pragma unroll
+        for (int b = 0; b < 2; ++b) {
+            const Frag d = columns_of(&sh.dz1[0][16 * b][0], &sh.dz1[1][16 * b][0], HP, 32 * ub);
+#pragma unroll
+            for (int t = 0; t < CT; ++t) gw1[t] = product(d, columns_of(&sh.xs[of][0][16 * b][0], &sh.xs[of][1][16 * b][0], XP, 32 * t), gw1[t]);
+#pragma unroll
+            for (int e = 0; e < 8; ++e) gb1 = __builtin_fmaf((float)d.hi[e], one, __builtin_fmaf((float)d.lo[e], one, gb1));
+            if (EXTRA)
+#pragma unroll
+                for (int e = 0; e < 8; ++e) {
+                    const float by = sh.share[of][16 * b + 8 * hh + e];
+                    gsm = __builtin_fmaf((float)d.hi[e], by, __builtin_fmaf((float)d.lo[e], by, gsm));
+                }
         }
     };
-    // bias, ReLU and dropout of this lane's 16 units of one layer
-    auto activate = [&](const floatx16 &z, float (&h)[16], const float *bias, const float share_here, long long sample, unsigned layer) {
-#pragma unroll
-        for (int g = 0; g < 2; ++g) {
-            Words4 bits;
-            if (a.drop) bits = drop_bits(a.rule, (unsigned long long)sample * (H / 8) + (u0 + 16 * g) / 8, layer);
-#pragma unroll
-            for (int e = 0; e < 8; ++e) {
-                float v = z[8 * g + e] + bias[u0 + 16 * g + e];
-                if (layer == 0 && a.W1sm) v = fmaf(share_here, vec[4 * H + u0 + 16 * g + e], v);
-                v = relu(v);
-                if (a.drop) v = drop_keeps(a.rule, bits, e) ? v * factor : 0.0f;
-                h[8 * g + e] = v;
-            }
+    meet();
+    for (int it = 0; it < mine; ++it) {
+        const bool more = it + 1 < mine;
+        if (more) { fetch(it + 1); look(it + 2); }
+        if (GRAD && it > 0) add_w1((it + 1) & 1);
+        meet();
+        if (more) {
+            stage(it + 1);
+            if (a.drop) draw(it + 1, 0);
         }
-    };
-    auto put = [&](float *to, const float (&h)[16]) {
-#pragma unroll
-        for (int g = 0; g < 2; ++g)
-#pragma unroll
-            for (int q = 0; q < 2; ++q)
-                *(float4 *)(to + mine * PITCH + u0 + 16 * g + 4 * q) = make_float4(h[8 * g + 4 * q], h[8 * g + 4 * q + 1], h[8 * g + 4 * q + 2], h[8 * g + 4 * q + 3]);
-    };
-
-    const long long tiles = (a.count + T - 1) / T;
-    for (long long tile = blockIdx.x; tile < tiles; tile += gridDim.x) {
-        __syncthreads();                                    // everybody is done with the last samples
-        if (tid < T) {
-            const long long s = tile * T + tid;
-            int i = -1, j = -1;
-            if (s < a.count) { i = a.index[0][s]; j = a.index[1][s]; }
-            // a sample that names no pair has no part in anything
-            if (i < 0 || i >= a.rows[0] || j < 0 || j >= a.rows[1]) i = j = -1;
-            at_on[tid] = i;
-            at_off[tid] = j;
-            const float none = __builtin_nanf("");
-            target[tid] = i >= 0 && a.target[0] ? a.target[0][s] : none;
-            target_slow[tid] = i >= 0 && a.target[1] ? a.target[1][s] : none;
-            share[tid] = i >= 0 && a.W1sm ? fminf(1.0f - a.X[0][(size_t)i * a.F + a.sm_feature[0]], a.X[1][(size_t)j * a.F + a.sm_feature[1]]) : 0.0f;
-        }
-        __syncthreads();
-        {   // moments of the samples' feature rows, 2 T of them, by THREADS / (2 T) neighbouring lanes each
-            constexpr int EACH = THREADS / (2 * T);
-            const int r = tid / EACH, sub = tid % EACH, side = r & 1;
-            const int at = side ? at_off[r >> 1] : at_on[r >> 1];
-            float2 m = make_float2(0.0f, 1.0f);
-            if (a.norm && at >= 0) {                        // (the lanes of a row agree)
-                const float *x = a.X[side] + (size_t)at * a.F;
-                float sum = 0.0f, squares = 0.0f;
-                for (int f = sub; f < a.F; f += EACH) sum += x[f];
-                m.x = group_sum<EACH>(sum) / (float)a.F;
-                for (int f = sub; f < a.F; f += EACH) { const float d = x[f] - m.x; squares = fmaf(d, d, squares); }
-                m.y = 1.0f / sqrtf(group_sum<EACH>(squares) / (float)a.F + a.eps);
-            }
-            if (sub == 0) moments[r] = m;
-        }
-        __syncthreads();
-        floatx16 z;
-#pragma unroll
-        for (int e = 0; e < 16; ++e) z[e] = 0.0f;
-        for (int c = 0; c < chunks; ++c) {
-            if (c > 0) __syncthreads();
-            stage(c);
-            __syncthreads();
-            const int quads = (a.padded - c * FIT_CHUNK < FIT_CHUNK ? a.padded - c * FIT_CHUNK : FIT_CHUNK) / 8;
-            for (int q = 0; q < quads; ++q) {
-                const float4 w = *(const float4 *)(a.W1 + (size_t)unit * a.padded + c * FIT_CHUNK + 8 * q + 4 * hh);
-                const float4 x = *(const float4 *)(xs + mine * XP + 8 * q + 4 * hh);
-                z = __builtin_amdgcn_mfma_f32_32x32x2f32(w.x, x.x, z, 0, 0, 0);
-                z = __builtin_amdgcn_mfma_f32_32x32x2f32(w.y, x.y, z, 0, 0, 0);
-                z = __builtin_amdgcn_mfma_f32_32x32x2f32(w.z, x.z, z, 0, 0, 0);
-                z = __builtin_amdgcn_mfma_f32_32x32x2f32(w.w, x.w, z, 0, 0, 0);
-            }
-        }
-        const long long sample = tile * T + mine;
-        const bool real = at_on[mine] >= 0;
-        float h1[16], h2[16];
-        activate(z, h1, vec, share[mine], sample, 0);
-        put(act, h1);
-        __syncthreads();
-#pragma unroll
-        for (int e = 0; e < 16; ++e) z[e] = 0.0f;
-        for (int q = 0; q < QUADS; ++q) {
-            const float4 w = *(const float4 *)(w2 + unit * PITCH + 8 * q + 4 * hh);
-            const float4 x = *(const float4 *)(act + mine * PITCH + 8 * q + 4 * hh);
-            z = __builtin_amdgcn_mfma_f32_32x32x2f32(w.x, x.x, z, 0, 0, 0);
-            z = __builtin_amdgcn_mfma_f32_32x32x2f32(w.y, x.y, z, 0, 0, 0);
-            z = __builtin_amdgcn_mfma_f32_32x32x2f32(w.z, x.z, z, 0, 0, 0);
-            z = __builtin_amdgcn_mfma_f32_32x32x2f32(w.w, x.w, z, 0, 0, 0);
-        }
-        activate(z, h2, vec + H, 0.0f, sample, 1);
-        float zp = 0.0f, zs = 0.0f;
-#pragma unroll
-        for (int g = 0; g < 2; ++g)
-#pragma unroll
-            for (int e = 0; e < 8; ++e) {
-                zp = fmaf(vec[2 * H + u0 + 16 * g + e], h2[8 * g + e], zp);
-                if (a.W3[1]) zs = fmaf(vec[3 * H + u0 + 16 * g + e], h2[8 * g + e], zs);
-            }
-        zp = other_half(zp);
-        zs = other_half(zs);
-        if (hh == 0) { part[ub * T + mine] = zp; part[(UB + ub) * T + mine] = zs; }
-        __syncthreads();
-        zp = b3; zs = b3s;
-#pragma unroll
-        for (int k = 0; k < UB; ++k) { zp += part[k * T + mine]; zs += part[(UB + k) * T + mine]; }
-        const float y = 1.0f / (1.0f + expf(-zp)), ys = 1.0f / (1.0f + expf(-zs));
-        const bool speaks = ub == 0 && hh == 0 && blockIdx.y == 0;      // for its sample, among the wavefronts and passes that hold it
-        if (speaks && sample < a.count) {
-            if (a.sigma[0]) a.sigma[0][sample] = real ? y : 0.0f;
-            if (a.sigma[1]) a.sigma[1][sample] = real ? ys : 0.0f;
-        }
-        // what nobody has measured (a NaN) has no part in the loss
-        const float t0 = target[mine], t1 = target_slow[mine];
-        const float miss = t0 == t0 ? y - t0 : 0.0f, miss_slow = t1 == t1 ? ys - t1 : 0.0f;
-        if (speaks) loss += fmaf(miss, miss, miss_slow * miss_slow);
+        meet();
+        if (more && a.drop) draw(it + 1, 1);
         if (!GRAD) continue;
-        const float dz = t0 == t0 ? 2.0f * a.scale * miss * y * (1.0f - y) : 0.0f;
-        const float dzs = t1 == t1 ? 2.0f * a.scale * miss_slow * ys * (1.0f - ys) : 0.0f;
-        if (speaks) { gb3 += dz; gb3s += dzs; }
-        float d[16];
+        meet();
 #pragma unroll
-        for (int g = 0; g < 2; ++g)
+        for (int b = 0; b < 2; ++b) {
+            const Frag d = columns_of(&sh.dz2[0][16 * b][0], &sh.dz2[1][16 * b][0], HP, 32 * ub);
 #pragma unroll
-            for (int e = 0; e < 8; ++e) {
-                const int k = 8 * g + e;
-                float v = dz * vec[2 * H + u0 + 16 * g + e];
-                gw3[k] = fmaf(dz, h2[k], gw3[k]);
-                if (a.W3[1]) {
-                    v = fmaf(dzs, vec[3 * H + u0 + 16 * g + e], v);
-                    gw3s[k] = fmaf(dzs, h2[k], gw3s[k]);
-                }
-                d[k] = h2[k] > 0.0f ? v * factor : 0.0f;
-                gb2[k] += d[k];
-            }
-        put(back, d);
-        __syncthreads();
+            for (int t = 0; t < UB; ++t) gw2[t] = product(d, columns_of(&sh.d1[0][16 * b][0], &sh.d1[1][16 * b][0], HP, 32 * t), gw2[t]);
 #pragma unroll
-        for (int e = 0; e < 16; ++e) z[e] = 0.0f;
-        for (int q = 0; q < QUADS; ++q) {                   // W2^T dz2
-            const float *w = w2 + (8 * q + 4 * hh) * PITCH + unit;
-            const float4 x = *(const float4 *)(back + mine * PITCH + 8 * q + 4 * hh);
-            z = __builtin_amdgcn_mfma_f32_32x32x2f32(w[0], x.x, z, 0, 0, 0);
-            z = __builtin_amdgcn_mfma_f32_32x32x2f32(w[PITCH], x.y, z, 0, 0, 0);
-            z = __builtin_amdgcn_mfma_f32_32x32x2f32(w[2 * PITCH], x.z, z, 0, 0, 0);
-            z = __builtin_amdgcn_mfma_f32_32x32x2f32(w[3 * PITCH], x.w, z, 0, 0, 0);
+            for (int e = 0; e < 8; ++e) gb2 = __builtin_fmaf((float)d.hi[e], one, __builtin_fmaf((float)d.lo[e], one, gb2));
         }
-#pragma unroll
-        for (int k = 0; k < 16; ++k) {
-            d[k] = h1[k] > 0.0f ? z[k] * factor : 0.0f;
-            gb1[k] += d[k];
-            if (a.W1sm) gsm[k] = fmaf(share[mine], d[k], gsm[k]);
-        }
-        // sums over samples: the lower half of a wavefront takes sample 16 b + i, the upper one 16 b + 8 + i
-        for (int b = 0; b < T / 16; ++b)
-#pragma unroll
-            for (int i = 0; i < 8; ++i) {
-                const int s = (16 * b + i + 8 * hh) * PITCH;
-                const float v = back[s + 32 * ub + nn];
-#pragma unroll
-                for (int t = 0; t < UB / 2; ++t)
-                    gw2[t] = __builtin_amdgcn_mfma_f32_32x32x2f32(v, act[s + 32 * (sh + 2 * t) + nn], gw2[t], 0, 0, 0);
-            }
-        __syncthreads();                                    // act has been read
-        put(act, d);
-        __syncthreads();
-#pragma unroll
-        for (int t = 0; t < GT; ++t) {
-            const int c = pass_chunk + t;
-            if (c >= chunks) break;
-            if (chunks > 1) {
-                if (t > 0) __syncthreads();
-                stage(c);
-                __syncthreads();
-            }
-            if (c * FIT_CHUNK + 32 * sh >= a.padded) continue;      // (the last chunk may be half as wide)
-            for (int b = 0; b < T / 16; ++b)
-#pragma unroll
-                for (int i = 0; i < 8; ++i) {
-                    const int s = 16 * b + i + 8 * hh;
-                    gw1[t] = __builtin_amdgcn_mfma_f32_32x32x2f32(act[s * PITCH + 32 * ub + nn], xs[s * XP + 32 * sh + nn], gw1[t], 0, 0, 0);
-                }
-        }
+        meet();
     }
-
-    // what this workgroup leaves
-    float *out = a.partial + (size_t)blockIdx.x * a.partial_step;
-    if (GRAD) {
-        const int row = 4 * hh;                             // rows 8 g + 4 hh + e of a tile are this lane's
+    if (!GRAD || !out) return;
+    add_w1((mine + 1) & 1);
+    const float by2 = 1.0f / (s_dz2 * s_d1), by1 = 1.0f / (s_dz1 * s_x);
 #pragma unroll
-        for (int t = 0; t < GT; ++t) {
-            const int c = (pass_chunk + t) * FIT_CHUNK + 32 * sh;
-            if (c >= a.padded) continue;
+    for (int e = 0; e < 16; ++e) {
+        const int k = 32 * ub + 8 * (e >> 2) + 4 * hh + (e & 3);
 #pragma unroll
-            for (int e = 0; e < 16; ++e) out[S::G + (size_t)(32 * ub + 8 * (e >> 2) + row + (e & 3)) * a.padded + c + nn] = gw1[t][e];
-        }
-        if (blockIdx.y > 0) return;
+        for (int t = 0; t < UB; ++t) out[S::W2 + k * H + 32 * t + nn] = gw2[t][e] * by2;
 #pragma unroll
-        for (int t = 0; t < UB / 2; ++t)
-#pragma unroll
-            for (int e = 0; e < 16; ++e) out[S::W2 + (32 * ub + 8 * (e >> 2) + row + (e & 3)) * H + 32 * (sh + 2 * t) + nn] = gw2[t][e];
-        // sums of a unit over the lanes that hold it, then over the two wavefronts that do
-        float *sums = act;                                  // [5][2][H]
-        __syncthreads();
-#pragma unroll
-        for (int k = 0; k < 16; ++k) {
-            const float v[5] = {group_sum<32>(gb1[k]), group_sum<32>(gb2[k]), group_sum<32>(gw3[k]), group_sum<32>(gw3s[k]), group_sum<32>(gsm[k])};
-#pragma unroll
-            for (int q = 0; q < 5; ++q)
-                if (nn == 0) sums[(2 * q + sh) * H + u0 + (k >> 3) * 16 + (k & 7)] = v[q];
-        }
-        __syncthreads();
-        for (int e = tid; e < 5 * H; e += THREADS) out[S::B1 + e] = sums[(2 * (e / H)) * H + e % H] + sums[(2 * (e / H) + 1) * H + e % H];
-        __syncthreads();
+        for (int t = 0; t < CT; ++t) out[S::G + k * (32 * CT) + 32 * t + nn] = gw1[t][e] * by1;
     }
-    if (a.partial) {
-        const float v[3] = {group_sum<64>(gb3), group_sum<64>(gb3s), group_sum<64>(loss)};
-        if (lane == 0 && ub == 0)
-#pragma unroll
-            for (int q = 0; q < 3; ++q) part[3 * sh + q] = v[q];
-        __syncthreads();
-        if (tid < 3) out[S::REST + tid] = part[tid] + part[3 + tid];
+    gb1 = both_halves(gb1) / s_dz1;
+    gb2 = both_halves(gb2) / s_dz2;
+    gsm = EXTRA ? both_halves(gsm) / s_dz1 : 0.0f;
+    if (hh == 0) {
+        out[S::B1 + 32 * ub + nn] = gb1;
+        out[S::B2 + 32 * ub + nn] = gb2;
+        out[S::SM + 32 * ub + nn] = gsm;
     }
-}
-
-// Layer 1 with the norm's weight and bias folded in, its rows padded with zeros: a wavefront for each hidden unit.
-__global__ __launch_bounds__(64) void fold_kernel(const float *W1, const float *b1, const float *g, const float *beta, int columns, int padded, float *W, float *b)
-{
-    const int k = blockIdx.x;
-    float sum = 0.0f;
-    for (int c = threadIdx.x; c < padded; c += 64) {
-        float v = 0.0f;
-        if (c < columns) {
-            v = W1[(size_t)k * columns + c];
-            if (g) { sum = fmaf(v, beta[c], sum); v *= g[c]; }
-        }
-        W[(size_t)k * padded + c] = v;
-    }
-    sum = group_sum<64>(sum);
-    if (threadIdx.x == 0) b[k] = b1[k] + sum;
 }
 
 // Sums of what the workgroups left: value v goes where it belongs.
 struct FitOut {
     float *W1, *b1, *W2, *b2, *W3, *b3, *W3s, *b3s, *W1sm, *loss, *G;
-    int H, columns, padded, norm, parts;
+    int H, F, padded, half, norm, parts;
     float scale;
 };
 constexpr int FIT_SUM_VALUES = 64, FIT_SUM_SLICES = 16;
@@ -386,6 +647,7 @@ __global__ __launch_bounds__(FIT_SUM_VALUES * FIT_SUM_SLICES) void fit_sum_kerne
     __syncthreads();
     if (slice > 0 || v >= values) return;
     for (int k = 1; k < FIT_SUM_SLICES; ++k) s += sums[k][place];
+    s *= o.scale;
     const int H = o.H;
     int at = v;
     if (at < H * H) { o.W2[at] = s; return; }
@@ -399,27 +661,27 @@ __global__ __launch_bounds__(FIT_SUM_VALUES * FIT_SUM_SLICES) void fit_sum_kerne
     if (at < 4) {
         if (at == REST_B3 && o.b3) *o.b3 = s;
         if (at == REST_B3S && o.b3s) *o.b3s = s;
-        if (at == REST_LOSS && o.loss) *o.loss = s * o.scale;
+        if (at == REST_LOSS && o.loss) *o.loss = s;
         return;
     }
     at -= 4;
-    const int k = at / o.padded, c = at % o.padded;
+    const int k = at / o.padded, c = at % o.padded, side = c >= o.half, f = c - side * o.half;
     if (o.norm) o.G[at] = s;
-    else if (c < o.columns) o.W1[(size_t)k * o.columns + c] = s;
+    else if (f < o.F) o.W1[(size_t)k * 2 * o.F + side * o.F + f] = s;
 }
 
 // dW1 = G diag g + h beta^T, dg_f = sum_k W1[k, f] G[k, f], dbeta = W1^T h.
 constexpr int UNFOLD_SLICES = 16;
 
 __global__ __launch_bounds__(64 * UNFOLD_SLICES) void unfold_kernel(const float *W1, const float *G, const float *h, const float *g, const float *beta, int H,
-                                                                    int columns, int padded, float *dW1, float *dg, float *dbeta)
+                                                                    int F, int padded, int half, float *dW1, float *dg, float *dbeta)
 {
     __shared__ float sums[2][UNFOLD_SLICES][64];
-    const int lane = threadIdx.x % 64, slice = threadIdx.x / 64, c = blockIdx.x * 64 + lane;
+    const int lane = threadIdx.x % 64, slice = threadIdx.x / 64, c = blockIdx.x * 64 + lane, columns = 2 * F, from = c < F ? c : half + c - F;
     float weight = 0.0f, bias = 0.0f;
     if (c < columns)
         for (int k = slice; k < H; k += UNFOLD_SLICES) {
-            const float G1 = G[(size_t)k * padded + c], W = W1[(size_t)k * columns + c];
+            const float G1 = G[(size_t)k * padded + from], W = W1[(size_t)k * columns + c];
             dW1[(size_t)k * columns + c] = fmaf(G1, g[c], h[k] * beta[c]);
             weight = fmaf(W, G1, weight);
             bias = fmaf(W, h[k], bias);
@@ -440,47 +702,58 @@ __global__ void clear_kernel(float *p, int count)
     if (i < count) p[i] = 0.0f;
 }
 
-struct FitPlan {
-    int H, columns, padded, passes, tiles_each, grid;
-    int values(bool grad) const { return (H == 64 ? FitSums<64>::G : FitSums<128>::G) + (grad ? H * padded : 0); }
-    long long step(bool grad) const { return (values(grad) + 15) & ~15; }
-};
 
 FitPlan fit_plan(const mf_ctx *ctx, const mf_predictor *p, long long count)
 {
     FitPlan f{};
     f.H = p->H;
     f.columns = 2 * p->F;
-    f.padded = (f.columns + 31) & ~31;
-    const int chunks = (f.padded + FIT_CHUNK - 1) / FIT_CHUNK, most = FIT_PASS_TILES / 2;
-    f.passes = (chunks + most - 1) / most;
-    f.tiles_each = chunks == 1 ? 1 : chunks == 2 ? 2 : most;
-    const long long tiles = (count + FIT_ROWS - 1) / FIT_ROWS;
-    const long long units = (ctx->n_cus > 0 ? ctx->n_cus : 256) * (p->H == 64 ? 2 : 1);
+    f.wide = p->F >= FIT_WIDE_FROM;
+    if (f.wide) {
+        mf_plan_wide(ctx, count, &f);
+        return f;
+    }
+    f.half = (p->F + 15) & ~15;
+    f.padded = 2 * f.half;
+    f.passes = 1;
+    f.tiles = f.padded / 32;
+    const long long tiles = (count + FIT_ROWS - 1) / FIT_ROWS, units = (ctx->n_cus > 0 ? ctx->n_cus : 256) * (p->H == 64 ? 2 : 1);
     f.grid = (int)(tiles < units ? tiles : units);
     return f;
 }
 
-template <int H, int GT, bool GRAD>
+// Where the folded layer 1 and what goes with it lie in the context's scratch (floats).
+constexpr int FOLD_BIAS = 128 * 512, FOLD_NORM1 = FOLD_BIAS + 128, FOLD_NORM2 = FOLD_NORM1 + 128, FOLD_RANGES = FOLD_NORM2 + 128, FOLD_SCALE = FOLD_RANGES + 2 * FIT_RANGE_PARTS;
+static_assert(FOLD_SCALE < MF_FIT_SCRATCH, "scratch");
+
+template <int H, int CT, bool GRAD, bool EXTRA>
 int launch_fit(mf_ctx *ctx, const FitArgs &a, const FitPlan &f)
 {
-    const unsigned flag = 1u << (21 + (H == 128 ? 4 : 0) + (GRAD ? GT / 2 + 1 : 0));
-    if (!(ctx->kernels_configured & flag)) {
-        MF_HIP(hipFuncSetAttribute((const void *)fit_kernel<H, GT, GRAD>, hipFuncAttributeMaxDynamicSharedMemorySize, (int)fit_lds_bytes<H>(GRAD)));
-        ctx->kernels_configured |= flag;
+    const int bytes = (int)sizeof(FitShared<H, CT, GRAD>);
+    static_assert(sizeof(FitShared<H, CT, GRAD>) <= 160 * 1024, "LDS");
+    const unsigned flag = 1u << ((H == 128 ? 16 : 0) + (GRAD ? 8 : 0) + (EXTRA ? 4 : 0) + CT - 1);
+    if (!(ctx->fit_configured & flag)) {
+        MF_HIP(hipFuncSetAttribute((const void *)fit_kernel<H, CT, GRAD, EXTRA>, hipFuncAttributeMaxDynamicSharedMemorySize, bytes));
+        ctx->fit_configured |= flag;
     }
-    hipLaunchKernelGGL((fit_kernel<H, GT, GRAD>), dim3(f.grid, GRAD ? f.passes : 1), dim3(H * 4), fit_lds_bytes<H>(GRAD), ctx->stream, a);
+    hipLaunchKernelGGL((fit_kernel<H, CT, GRAD, EXTRA>), dim3(f.grid), dim3(H * 4), bytes, ctx->stream, a, ctx->fit_W1 + FOLD_SCALE, ctx->fit_W1 + FOLD_NORM1,
+                       ctx->fit_W1 + FOLD_NORM2, ctx->fit_W1 + FOLD_RANGES);
     MF_HIP(hipGetLastError());
     return MF_OK;
+}
+
+template <int H, bool GRAD, bool EXTRA>
+int launch_fit_tiles(mf_ctx *ctx, const FitArgs &a, const FitPlan &f)
+{
+    if (f.tiles == 1) return launch_fit<H, 1, GRAD, EXTRA>(ctx, a, f);
+    return f.tiles == 2 ? launch_fit<H, 2, GRAD, EXTRA>(ctx, a, f) : launch_fit<H, 3, GRAD, EXTRA>(ctx, a, f);
 }
 
 template <int H>
 int launch_fit_for(mf_ctx *ctx, const FitArgs &a, const FitPlan &f, bool grad)
 {
-    if (!grad) return launch_fit<H, 1, false>(ctx, a, f);
-    if (f.tiles_each == 1) return launch_fit<H, 1, true>(ctx, a, f);
-    if (f.tiles_each == 2) return launch_fit<H, 2, true>(ctx, a, f);
-    return launch_fit<H, 4, true>(ctx, a, f);
+    if (a.W3[1] || a.W1sm) return grad ? launch_fit_tiles<H, true, true>(ctx, a, f) : launch_fit_tiles<H, false, true>(ctx, a, f);
+    return grad ? launch_fit_tiles<H, true, false>(ctx, a, f) : launch_fit_tiles<H, false, false>(ctx, a, f);
 }
 
 bool whole_floats(const void *p) { return ((uintptr_t)p & 3u) == 0; }
@@ -493,26 +766,33 @@ int run_fit(mf_ctx *ctx, const mf_predictor *p, const float *d_on, int n, const 
     FitArgs a{};
     a.X[0] = d_on; a.X[1] = d_off;
     a.rows[0] = n; a.rows[1] = m;
-    a.F = p->F; a.columns = f.columns; a.padded = f.padded;
+    a.F = p->F; a.columns = f.columns; a.padded = f.padded; a.half = f.half;
     a.index[0] = s->d_on; a.index[1] = s->d_off;
     a.target[0] = s->d_target; a.target[1] = s->d_target_slow;
     a.sigma[0] = d_sigma; a.sigma[1] = d_sigma_slow;
     a.count = s->count;
-    a.W1 = ctx->fit_W1; a.b1 = ctx->fit_W1 + 128 * FIT_COLUMNS_MAX;
+    a.W1 = ctx->fit_W1; a.b1 = ctx->fit_W1 + FOLD_BIAS;
     a.W2 = p->d_W2; a.b2 = p->d_b2;
     a.W3[0] = p->d_W3; a.W3[1] = p->d_W3_slow;
     a.b3[0] = p->d_b3; a.b3[1] = p->d_b3_slow;
     a.W1sm = p->d_W1sm;
     a.norm = p->d_ln_w != nullptr; a.eps = p->ln_eps;
     a.sm_feature[0] = p->sm_on_feature; a.sm_feature[1] = p->sm_off_feature;
-    a.scale = scale;
     a.drop = rule && rule->limit > 0;
     if (a.drop) { a.rule = *rule; a.step = (const unsigned long long *)d_step; }
     a.partial = (float *)d_work;
     a.partial_step = f.step(g != nullptr);
-    hipLaunchKernelGGL(fold_kernel, dim3(f.H), dim3(64), 0, ctx->stream, p->d_W1, p->d_b1, p->d_ln_w, p->d_ln_b, f.columns, f.padded, ctx->fit_W1, ctx->fit_W1 + 128 * FIT_COLUMNS_MAX);
+    FoldArgs w{};
+    w.W1 = p->d_W1; w.b1 = p->d_b1; w.g = p->d_ln_w; w.beta = p->d_ln_b;
+    w.H = f.H; w.F = p->F; w.padded = f.padded; w.half = f.half; w.wide = f.wide;
+    w.image = ctx->fit_W1; w.bias = ctx->fit_W1 + FOLD_BIAS; w.scale = ctx->fit_W1 + FOLD_SCALE;
+    w.norm1 = ctx->fit_W1 + FOLD_NORM1; w.norm2 = ctx->fit_W1 + FOLD_NORM2; w.ranges = ctx->fit_W1 + FOLD_RANGES;
+    for (int k = 0; k < 2; ++k) { w.target[k] = a.target[k]; w.X[k] = a.X[k]; w.index[k] = a.index[k]; w.rows[k] = a.rows[k]; }
+    w.count = a.count;
+    w.features = f.wide || (a.norm && !a.W1sm) ? 0 : 2 * s->count < (long long)n + m ? 2 : 1;
+    hipLaunchKernelGGL(fold_kernel, dim3(f.H / 4 + (f.wide ? 0 : FIT_RANGE_PARTS)), dim3(256), 0, ctx->stream, w);
     MF_HIP(hipGetLastError());
-    const int rc = f.H == 64 ? launch_fit_for<64>(ctx, a, f, g != nullptr) : launch_fit_for<128>(ctx, a, f, g != nullptr);
+    const int rc = f.wide ? mf_launch_wide(ctx, a, f, g != nullptr) : f.H == 64 ? launch_fit_for<64>(ctx, a, f, g != nullptr) : launch_fit_for<128>(ctx, a, f, g != nullptr);
     if (rc != MF_OK || !a.partial) return rc;
     FitOut o{};
     if (g) {
@@ -522,13 +802,13 @@ int run_fit(mf_ctx *ctx, const mf_predictor *p, const float *d_on, int n, const 
     }
     o.loss = d_loss;
     o.G = a.partial + (size_t)f.grid * a.partial_step;
-    o.H = f.H; o.columns = f.columns; o.padded = f.padded; o.norm = a.norm; o.parts = f.grid; o.scale = scale;
+    o.H = f.H; o.F = p->F; o.padded = f.padded; o.half = f.half; o.norm = a.norm; o.parts = f.grid; o.scale = scale;
     const int values = f.values(g != nullptr), first = g ? 0 : values - 4;
     hipLaunchKernelGGL(fit_sum_kernel, dim3((values - first + FIT_SUM_VALUES - 1) / FIT_SUM_VALUES), dim3(FIT_SUM_VALUES * FIT_SUM_SLICES), 0, ctx->stream,
                        a.partial, a.partial_step, first, values, o);
     if (g && a.norm)
         hipLaunchKernelGGL(unfold_kernel, dim3((f.columns + 63) / 64), dim3(64 * UNFOLD_SLICES), 0, ctx->stream, p->d_W1, o.G, g->d_b1, p->d_ln_w, p->d_ln_b,
-                           f.H, f.columns, f.padded, g->d_W1, g->d_ln_w, g->d_ln_b);
+                           f.H, p->F, f.padded, f.half, g->d_W1, g->d_ln_w, g->d_ln_b);
     MF_HIP(hipGetLastError());
     return MF_OK;
 }

@@ -1,0 +1,60 @@
+// What the kernels of a fit share (fit.hip, fit_wide.hip).
+#pragma once
+#include "internal.h"
+#include "philox.h"
+#include "row_sums.h"
+#include <math.h>
+
+typedef float floatx16 __attribute__((ext_vector_type(16)));
+
+constexpr int FIT_WIDE_FROM = 49;                           // features a workload from which on fit_wide.hip takes over
+constexpr int FIT_RANGE_PARTS = 64;                         // workgroups that look for the largest target and feature
+
+struct FitArgs {
+    const float *X[2];
+    int rows[2], F, columns, padded, half;                  // columns = 2F; laid out as [0, F) and [half, half + F) of `padded` ones
+    const int32_t *index[2];
+    const float *target[2];                                 // throughput, slowdown (null: not trained)
+    float *sigma[2];                                        // (null: not wanted)
+    long long count;
+    const float *W1, *b1;                                   // layer 1 with the norm folded in (see fold_kernel)
+    const float *W2, *b2, *W3[2], *b3[2], *W1sm;            // ([1] and W1sm may be null)
+    int norm, sm_feature[2];
+    float eps;
+    int drop;
+    DropRule rule;
+    const unsigned long long *step;
+    float *partial;
+    long long partial_step;
+};
+
+// What a workgroup leaves, one after the other.
+template <int H>
+struct FitSums {
+    static constexpr int W2 = 0, B1 = H * H, B2 = B1 + H, W3 = B2 + H, W3S = W3 + H, SM = W3S + H, REST = SM + H, G = REST + 4;
+};
+enum { REST_B3 = 0, REST_B3S, REST_LOSS };
+
+struct FitPlan {
+    int H, columns, padded, half, passes, tiles, grid;      // tiles: of 32 columns that a pass over the samples keeps gradients of, for each wavefront
+    bool wide;
+    int values(bool grad) const { return (H == 64 ? FitSums<64>::G : FitSums<128>::G) + (grad ? H * padded : 0); }
+    long long step(bool grad) const { return (values(grad) + 15) & ~15; }
+};
+
+void mf_plan_wide(const mf_ctx *ctx, long long count, FitPlan *f);
+int mf_launch_wide(mf_ctx *ctx, const FitArgs &a, const FitPlan &f, bool grad);
+
+namespace {
+
+// Row r of a 32-row tile of matrix results lies in lane half (r >> 2) & 1; read as unit tile_unit(r), what a lane holds of
+// a tile are the units 8 half .. 8 half + 7 and 16 + 8 half .. 16 + 8 half + 7: eight that share a counter.
+__device__ __forceinline__ int tile_unit(int r) { return (r & 0x13) | (r & 4) << 1 | (r & 8) >> 1; }
+
+__device__ __forceinline__ float both_halves(float v)
+{
+    const auto s = __builtin_amdgcn_permlane32_swap(__float_as_uint(v), __float_as_uint(v), false, false);
+    return __uint_as_float(s[0]) + __uint_as_float(s[1]);
+}
+
+}  // namespace

@@ -1,0 +1,332 @@
+// The pass over the samples of a predictor of many features (49 to 256 a workload), in float32 products: features are staged 64 columns at a time, twice a
+// sample, and gradients of layer 1 are kept for 256 columns at a time, which is as many as there are accumulators for: more take another pass over
+// the samples each.  See fit.hip for what is computed.
+#include "fit_parts.h"
+
+namespace {
+
+constexpr int FIT_ROWS = 64, FIT_CHUNK = 64;                // samples a workgroup takes at a time; features staged at a time
+
+// max(v, 0) that keeps a NaN: a fit that has diverged shows.
+__device__ __forceinline__ float relu(float v) { return v < 0.0f ? 0.0f : v; }
+
+template <int H>
+constexpr size_t wide_lds_bytes(bool grad)
+{
+    return sizeof(float) * ((size_t)H * (H + 4) + FIT_ROWS * (FIT_CHUNK + 4) + (size_t)FIT_ROWS * (H + 4) * (grad ? 2 : 1) +
+                            2 * (H / 32) * FIT_ROWS + FIT_ROWS * 5 + 4 * FIT_ROWS + 5 * H);
+}
+
+template <int H, int GT, bool GRAD>
+__global__ __launch_bounds__(H * 4) void wide_kernel(FitArgs a)
+{
+    constexpr int T = FIT_ROWS, PITCH = H + 4, XP = FIT_CHUNK + 4, UB = H / 32, THREADS = H * 4, QUADS = H / 8;
+    using S = FitSums<H>;
+    extern __shared__ __align__(16) float lds[];
+    float *w2 = lds, *xs = w2 + H * PITCH, *act = xs + T * XP, *back = act + T * PITCH;
+    float *part = back + (GRAD ? T * PITCH : 0), *target = part + 2 * UB * T, *target_slow = target + T, *share = target_slow + T;
+    int *at_on = (int *)(share + T), *at_off = at_on + T;
+    float2 *moments = (float2 *)(at_off + T);
+    float *vec = (float *)(moments + 2 * T);                // b1, b2, W3, W3 of the slowdown unit, W1sm
+    const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6, nn = lane & 31, hh = lane >> 5;
+    const int ub = wave % UB, sh = wave / UB;               // units 32 ub .. and samples 32 sh .. of the forward pass are this wavefront's
+    const int unit = 32 * ub + tile_unit(nn), mine = 32 * sh + nn, u0 = 32 * ub + 8 * hh;
+    if (a.step) { const unsigned long long s = *a.step; a.rule.s0 = (unsigned)s; a.rule.s1 = (unsigned)(s >> 32); }
+
+    for (int e = tid; e < H * H / 4; e += THREADS) *(float4 *)(w2 + e / (H / 4) * PITCH + e % (H / 4) * 4) = ((const float4 *)a.W2)[e];
+    for (int e = tid; e < H; e += THREADS) {
+        vec[e] = a.b1[e];
+        vec[H + e] = a.b2[e];
+        vec[2 * H + e] = a.W3[0][e];
+        vec[3 * H + e] = a.W3[1] ? a.W3[1][e] : 0.0f;
+        vec[4 * H + e] = a.W1sm ? a.W1sm[e] : 0.0f;
+    }
+    const float b3 = *a.b3[0], b3s = a.W3[1] ? *a.b3[1] : 0.0f;
+    const float factor = a.drop ? a.rule.factor : 1.0f;
+    const int chunks = (a.padded + FIT_CHUNK - 1) / FIT_CHUNK;
+    const int pass_chunk = blockIdx.y * GT;                 // this pass keeps gradients of layer 1 from this chunk on
+
+    floatx16 gw2[UB / 2], gw1[GT];
+    // sums of the 16 units of a half over the wavefront's samples: lane nn of a half keeps that of unit nn
+    float gb1 = 0.0f, gb2 = 0.0f, gw3 = 0.0f, gw3s = 0.0f, gsm = 0.0f, gb3 = 0.0f, gb3s = 0.0f, loss = 0.0f;
+    if (GRAD) {
+#pragma unroll
+        for (int e = 0; e < 16; ++e) {
+#pragma unroll
+            for (int t = 0; t < UB / 2; ++t) gw2[t][e] = 0.0f;
+#pragma unroll
+            for (int t = 0; t < GT; ++t) gw1[t][e] = 0.0f;
+        }
+    }
+    // features of columns 64 chunk .. 64 chunk + 63
+    auto stage = [&](const int chunk) {
+        for (int e = tid; e < T * FIT_CHUNK; e += THREADS) {
+            const int s = e / FIT_CHUNK, c = chunk * FIT_CHUNK + e % FIT_CHUNK, side = c >= a.F;
+            float v = 0.0f;
+            if (c < a.columns && at_on[s] >= 0) {
+                const float2 m = moments[2 * s + side];
+                v = (a.X[side][(size_t)(side ? at_off[s] : at_on[s]) * a.F + c - (side ? a.F : 0)] - m.x) * m.y;
+            }
+            xs[s * XP + e % FIT_CHUNK] = v;
+        }
+    };
+    // bias, ReLU and dropout of this lane's 16 units of one layer
+    auto activate = [&](const floatx16 &z, float (&h)[16], const float *bias, const float share_here, long long sample, unsigned layer) {
+#pragma unroll
+        for (int g = 0; g < 2; ++g) {
+            Words4 bits;
+            if (a.drop) bits = drop_bits(a.rule, (unsigned long long)sample * (H / 8) + (u0 + 16 * g) / 8, layer);
+#pragma unroll
+            for (int e = 0; e < 8; ++e) {
+                float v = z[8 * g + e] + bias[u0 + 16 * g + e];
+                if (layer == 0 && a.W1sm) v = fmaf(share_here, vec[4 * H + u0 + 16 * g + e], v);
+                v = relu(v);
+                if (a.drop) v = drop_keeps(a.rule, bits, e) ? v * factor : 0.0f;
+                h[8 * g + e] = v;
+            }
+        }
+    };
+    auto add_lane = [&](float &sum, const int k, const float v) {
+        const float all = group_sum<32>(v);
+        sum += nn == k ? all : 0.0f;
+    };
+    auto put = [&](float *to, const float (&h)[16]) {
+#pragma unroll
+        for (int g = 0; g < 2; ++g)
+#pragma unroll
+            for (int q = 0; q < 2; ++q)
+                *(float4 *)(to + mine * PITCH + u0 + 16 * g + 4 * q) = make_float4(h[8 * g + 4 * q], h[8 * g + 4 * q + 1], h[8 * g + 4 * q + 2], h[8 * g + 4 * q + 3]);
+    };
+
+    const long long tiles = (a.count + T - 1) / T;
+    for (long long tile = blockIdx.x; tile < tiles; tile += gridDim.x) {
+        __syncthreads();                                    // everybody is done with the last samples
+        if (tid < T) {
+            const long long s = tile * T + tid;
+            int i = -1, j = -1;
+            if (s < a.count) { i = a.index[0][s]; j = a.index[1][s]; }
+            // a sample that names no pair has no part in anything
+            if (i < 0 || i >= a.rows[0] || j < 0 || j >= a.rows[1]) i = j = -1;
+            at_on[tid] = i;
+            at_off[tid] = j;
+            const float none = __builtin_nanf("");
+            target[tid] = i >= 0 && a.target[0] ? a.target[0][s] : none;
+            target_slow[tid] = i >= 0 && a.target[1] ? a.target[1][s] : none;
+            share[tid] = i >= 0 && a.W1sm ? fminf(1.0f - a.X[0][(size_t)i * a.F + a.sm_feature[0]], a.X[1][(size_t)j * a.F + a.sm_feature[1]]) : 0.0f;
+        }
+        __syncthreads();
+        {   // moments of the samples' feature rows, 2 T of them, by THREADS / (2 T) neighbouring lanes each
+            constexpr int EACH = THREADS / (2 * T);
+            const int r = tid / EACH, sub = tid % EACH, side = r & 1;
+            const int at = side ? at_off[r >> 1] : at_on[r >> 1];
+            float2 m = make_float2(0.0f, 1.0f);
+            if (a.norm && at >= 0) {                        // (the lanes of a row agree)
+                const float *x = a.X[side] + (size_t)at * a.F;
+                float sum = 0.0f, squares = 0.0f;
+                for (int f = sub; f < a.F; f += EACH) sum += x[f];
+                m.x = group_sum<EACH>(sum) / (float)a.F;
+                for (int f = sub; f < a.F; f += EACH) { const float d = x[f] - m.x; squares = fmaf(d, d, squares); }
+                m.y = 1.0f / sqrtf(group_sum<EACH>(squares) / (float)a.F + a.eps);
+            }
+            if (sub == 0) moments[r] = m;
+        }
+        __syncthreads();
+        floatx16 z;
+#pragma unroll
+        for (int e = 0; e < 16; ++e) z[e] = 0.0f;
+        for (int c = 0; c < chunks; ++c) {
+            if (c > 0) __syncthreads();
+            stage(c);
+            __syncthreads();
+            const int quads = (a.padded - c * FIT_CHUNK < FIT_CHUNK ? a.padded - c * FIT_CHUNK : FIT_CHUNK) / 8;
+            for (int q = 0; q < quads; ++q) {
+                const float4 w = *(const float4 *)(a.W1 + (size_t)unit * a.padded + c * FIT_CHUNK + 8 * q + 4 * hh);
+                const float4 x = *(const float4 *)(xs + mine * XP + 8 * q + 4 * hh);
+                z = __builtin_amdgcn_mfma_f32_32x32x2f32(w.x, x.x, z, 0, 0, 0);
+                z = __builtin_amdgcn_mfma_f32_32x32x2f32(w.y, x.y, z, 0, 0, 0);
+                z = __builtin_amdgcn_mfma_f32_32x32x2f32(w.z, x.z, z, 0, 0, 0);
+                z = __builtin_amdgcn_mfma_f32_32x32x2f32(w.w, x.w, z, 0, 0, 0);
+            }
+        }
+        const long long sample = tile * T + mine;
+        const bool real = at_on[mine] >= 0;
+        float h1[16], h2[16];
+        activate(z, h1, vec, share[mine], sample, 0);
+        put(act, h1);
+        __syncthreads();
+#pragma unroll
+        for (int e = 0; e < 16; ++e) z[e] = 0.0f;
+        for (int q = 0; q < QUADS; ++q) {
+            const float4 w = *(const float4 *)(w2 + unit * PITCH + 8 * q + 4 * hh);
+            const float4 x = *(const float4 *)(act + mine * PITCH + 8 * q + 4 * hh);
+            z = __builtin_amdgcn_mfma_f32_32x32x2f32(w.x, x.x, z, 0, 0, 0);
+            z = __builtin_amdgcn_mfma_f32_32x32x2f32(w.y, x.y, z, 0, 0, 0);
+            z = __builtin_amdgcn_mfma_f32_32x32x2f32(w.z, x.z, z, 0, 0, 0);
+            z = __builtin_amdgcn_mfma_f32_32x32x2f32(w.w, x.w, z, 0, 0, 0);
+        }
+        activate(z, h2, vec + H, 0.0f, sample, 1);
+        float zp = 0.0f, zs = 0.0f;
+#pragma unroll
+        for (int g = 0; g < 2; ++g)
+#pragma unroll
+            for (int e = 0; e < 8; ++e) {
+                zp = fmaf(vec[2 * H + u0 + 16 * g + e], h2[8 * g + e], zp);
+                if (a.W3[1]) zs = fmaf(vec[3 * H + u0 + 16 * g + e], h2[8 * g + e], zs);
+            }
+        zp = both_halves(zp);
+        zs = both_halves(zs);
+        if (hh == 0) { part[ub * T + mine] = zp; part[(UB + ub) * T + mine] = zs; }
+        __syncthreads();
+        zp = b3; zs = b3s;
+#pragma unroll
+        for (int k = 0; k < UB; ++k) { zp += part[k * T + mine]; zs += part[(UB + k) * T + mine]; }
+        const float y = 1.0f / (1.0f + expf(-zp)), ys = 1.0f / (1.0f + expf(-zs));
+        const bool speaks = ub == 0 && hh == 0 && blockIdx.y == 0;      // for its sample, among the wavefronts and passes that hold it
+        if (speaks && sample < a.count) {
+            if (a.sigma[0]) a.sigma[0][sample] = real ? y : 0.0f;
+            if (a.sigma[1]) a.sigma[1][sample] = real ? ys : 0.0f;
+        }
+        // what nobody has measured (a NaN) has no part in the loss
+        const float t0 = target[mine], t1 = target_slow[mine];
+        const float miss = t0 == t0 ? y - t0 : 0.0f, miss_slow = t1 == t1 ? ys - t1 : 0.0f;
+        if (speaks) loss += fmaf(miss, miss, miss_slow * miss_slow);
+        if (!GRAD) continue;
+        const float dz = t0 == t0 ? 2.0f * miss * y * (1.0f - y) : 0.0f;        // (the caller's scale comes last)
+        const float dzs = t1 == t1 ? 2.0f * miss_slow * ys * (1.0f - ys) : 0.0f;
+        if (speaks) { gb3 += dz; gb3s += dzs; }
+        float d[16];
+#pragma unroll
+        for (int g = 0; g < 2; ++g)
+#pragma unroll
+            for (int e = 0; e < 8; ++e) {
+                const int k = 8 * g + e;
+                float v = dz * vec[2 * H + u0 + 16 * g + e];
+                add_lane(gw3, k, dz * h2[k]);
+                if (a.W3[1]) {
+                    v = fmaf(dzs, vec[3 * H + u0 + 16 * g + e], v);
+                    add_lane(gw3s, k, dzs * h2[k]);
+                }
+                d[k] = h2[k] > 0.0f ? v * factor : 0.0f;
+                add_lane(gb2, k, d[k]);
+            }
+        put(back, d);
+        __syncthreads();
+#pragma unroll
+        for (int e = 0; e < 16; ++e) z[e] = 0.0f;
+        for (int q = 0; q < QUADS; ++q) {                   // W2^T dz2
+            const float *w = w2 + (8 * q + 4 * hh) * PITCH + unit;
+            const float4 x = *(const float4 *)(back + mine * PITCH + 8 * q + 4 * hh);
+            z = __builtin_amdgcn_mfma_f32_32x32x2f32(w[0], x.x, z, 0, 0, 0);
+            z = __builtin_amdgcn_mfma_f32_32x32x2f32(w[PITCH], x.y, z, 0, 0, 0);
+            z = __builtin_amdgcn_mfma_f32_32x32x2f32(w[2 * PITCH], x.z, z, 0, 0, 0);
+            z = __builtin_amdgcn_mfma_f32_32x32x2f32(w[3 * PITCH], x.w, z, 0, 0, 0);
+        }
+#pragma unroll
+        for (int k = 0; k < 16; ++k) {
+            d[k] = h1[k] > 0.0f ? z[k] * factor : 0.0f;
+            add_lane(gb1, k, d[k]);
+            if (a.W1sm) add_lane(gsm, k, share[mine] * d[k]);
+        }
+        // sums over samples: the lower half of a wavefront takes sample 16 b + i, the upper one 16 b + 8 + i
+        for (int b = 0; b < T / 16; ++b)
+#pragma unroll
+            for (int i = 0; i < 8; ++i) {
+                const int s = (16 * b + i + 8 * hh) * PITCH;
+                const float v = back[s + 32 * ub + nn];
+#pragma unroll
+                for (int t = 0; t < UB / 2; ++t)
+                    gw2[t] = __builtin_amdgcn_mfma_f32_32x32x2f32(v, act[s + 32 * (sh + 2 * t) + nn], gw2[t], 0, 0, 0);
+            }
+        __syncthreads();                                    // act has been read
+        put(act, d);
+        __syncthreads();
+#pragma unroll
+        for (int t = 0; t < GT; ++t) {
+            const int c = pass_chunk + t;
+            if (c >= chunks) break;
+            if (chunks > 1) {
+                if (t > 0) __syncthreads();
+                stage(c);
+                __syncthreads();
+            }
+            if (c * FIT_CHUNK + 32 * sh >= a.padded) continue;      // (the last chunk may be half as wide)
+            for (int b = 0; b < T / 16; ++b)
+#pragma unroll
+                for (int i = 0; i < 8; ++i) {
+                    const int s = 16 * b + i + 8 * hh;
+                    gw1[t] = __builtin_amdgcn_mfma_f32_32x32x2f32(act[s * PITCH + 32 * ub + nn], xs[s * XP + 32 * sh + nn], gw1[t], 0, 0, 0);
+                }
+        }
+    }
+
+    // what this workgroup leaves
+    if (!a.partial) return;
+    float *out = a.partial + (size_t)blockIdx.x * a.partial_step;
+    if (GRAD) {
+        const int row = 4 * hh;                             // rows 8 g + 4 hh + e of a tile are this lane's
+#pragma unroll
+        for (int t = 0; t < GT; ++t) {
+            const int c = (pass_chunk + t) * FIT_CHUNK + 32 * sh;
+            if (c >= a.padded) continue;
+#pragma unroll
+            for (int e = 0; e < 16; ++e) out[S::G + (size_t)(32 * ub + 8 * (e >> 2) + row + (e & 3)) * a.padded + c + nn] = gw1[t][e];
+        }
+        if (blockIdx.y > 0) return;
+#pragma unroll
+        for (int t = 0; t < UB / 2; ++t)
+#pragma unroll
+            for (int e = 0; e < 16; ++e) out[S::W2 + (32 * ub + 8 * (e >> 2) + row + (e & 3)) * H + 32 * (sh + 2 * t) + nn] = gw2[t][e];
+        // sums of a unit over the lanes that hold it, then over the two wavefronts that do
+        float *sums = act;                                  // [5][2][H]
+        __syncthreads();
+        const float v[5] = {gb1, gb2, gw3, gw3s, gsm};
+#pragma unroll
+        for (int q = 0; q < 5; ++q)
+            if (nn < 16) sums[(2 * q + sh) * H + u0 + (nn >> 3) * 16 + (nn & 7)] = v[q];
+        __syncthreads();
+        for (int e = tid; e < 5 * H; e += THREADS) out[S::B1 + e] = sums[(2 * (e / H)) * H + e % H] + sums[(2 * (e / H) + 1) * H + e % H];
+        __syncthreads();
+    }
+    const float v[3] = {group_sum<64>(gb3), group_sum<64>(gb3s), group_sum<64>(loss)};
+    __syncthreads();
+    if (lane == 0 && ub == 0)
+#pragma unroll
+        for (int q = 0; q < 3; ++q) part[3 * sh + q] = v[q];
+    __syncthreads();
+    if (tid < 3) out[S::REST + tid] = part[tid] + part[3 + tid];
+}
+
+template <int H, int GT, bool GRAD>
+int launch_wide(mf_ctx *ctx, const FitArgs &a, const FitPlan &f)
+{
+    const unsigned flag = 1u << (21 + (H == 128 ? 2 : 0) + (GRAD ? 1 : 0));
+    if (!(ctx->kernels_configured & flag)) {
+        MF_HIP(hipFuncSetAttribute((const void *)wide_kernel<H, GT, GRAD>, hipFuncAttributeMaxDynamicSharedMemorySize, (int)wide_lds_bytes<H>(GRAD)));
+        ctx->kernels_configured |= flag;
+    }
+    hipLaunchKernelGGL((wide_kernel<H, GT, GRAD>), dim3(f.grid, GRAD ? f.passes : 1), dim3(H * 4), wide_lds_bytes<H>(GRAD), ctx->stream, a);
+    MF_HIP(hipGetLastError());
+    return MF_OK;
+}
+
+}  // namespace
+
+constexpr int FIT_WIDE_TILES = 4;
+
+void mf_plan_wide(const mf_ctx *ctx, long long count, FitPlan *f)
+{
+    f->half = f->columns / 2;
+    f->padded = (f->columns + 31) & ~31;
+    f->tiles = FIT_WIDE_TILES;
+    const int chunks = (f->padded + FIT_CHUNK - 1) / FIT_CHUNK;
+    f->passes = (chunks + FIT_WIDE_TILES - 1) / FIT_WIDE_TILES;
+    const long long tiles = (count + FIT_ROWS - 1) / FIT_ROWS, units = (ctx->n_cus > 0 ? ctx->n_cus : 256) * (f->H == 64 ? 2 : 1);
+    f->grid = (int)(tiles < units ? tiles : units);
+}
+
+int mf_launch_wide(mf_ctx *ctx, const FitArgs &a, const FitPlan &f, bool grad)
+{
+    if (f.H == 64) return grad ? launch_wide<64, FIT_WIDE_TILES, true>(ctx, a, f) : launch_wide<64, 1, false>(ctx, a, f);
+    return grad ? launch_wide<128, FIT_WIDE_TILES, true>(ctx, a, f) : launch_wide<128, 1, false>(ctx, a, f);
+}
+

@@ -24,6 +24,7 @@
 #define MF_MAX_DIM ((1 << MF_ID_BITS) - 2)
 #define MF_MAX_DUAL (1ll << 43)
 #define MF_MAX_TYPES 64
+#define MF_FIT_SCRATCH (128 * 512 + 1024)
 
 enum { T_PROJ = 0, T_PAIR, T_BID_BULK, T_BID_BULK_LAUNCHES, T_TRANSPOSE, T_DUALS, T_CERT, T_SOLVE,
        T_BID_BULK_BYTES, T_PAIR_EVALUATED, T_LIST_LAUNCHES, T_LISTS_MADE, T_LIST_SIDES_LEFT, T_LISTS_BY_COLUMN, T_COUNT = 16 };
@@ -234,7 +235,8 @@ struct mf_ctx : mf_options {
     int *score_queue;                   // device: next tasks of the pair kernel's launches, one a type, MF_PAIR_QUEUES counters each
     unsigned *score_range;              // device: largest magnitudes the scorer's fp16 pieces are scaled by (project_kernel)
     mf_cert_out *h_cert;
-    float *fit_W1;                      // device: [128][512] layer 1 with the norm folded in, and [128] its bias (fit.hip)
+    float *fit_W1;                      // device, MF_FIT_SCRATCH floats: layer 1 with the norm folded in, and what bounds a fit's values (fit.hip)
+    unsigned fit_configured;            // as kernels_configured, of the kernels of fit.hip
     // timing
     unsigned long long *times, *h_times;        // [AT_COUNT] device, pinned
     double clock_khz;               // of the clock they are in
