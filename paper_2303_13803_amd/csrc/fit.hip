@@ -22,8 +22,9 @@
 // activations pass between them through LDS.  The others ("sums") add up the gradients of weights, in accumulators that stay until there are no
 // more samples, and get the next samples ready: features, their norm, random bits.  A SIMD has one wavefront of either kind, so that the matrix
 // instructions of one run beside the arithmetic of the other:
-//     forward   layer 1 -> d1      layer 2 -> output      loss, dz2           W2^T dz2 -> dz1
-//     sums      G of the last      next features          next random bits    dW2
+//     forward   layer 1 -> d1        layer 2 -> output    loss, dz2        W2^T dz2 -> dz1
+//     sums      dW2, second half     G                    next features    dW2, first half      (either half: 16 samples)
+// so that the matrix pipe has something to do throughout; random bits for the next samples are drawn in all four stages.
 //
 // NaN: a ReLU that is one instruction turns it into 0, so what is not finite among the weights, or a sample's features, is added to the output as a NaN.
 #include "fit_parts.h"
@@ -32,6 +33,8 @@ typedef _Float16 half2v __attribute__((ext_vector_type(2)));
 typedef _Float16 half4v __attribute__((ext_vector_type(4)));
 typedef _Float16 half8v __attribute__((ext_vector_type(8)));
 typedef float float2v __attribute__((ext_vector_type(2)));
+typedef float float4v __attribute__((ext_vector_type(4), aligned(4)));
+typedef unsigned short ushort2v __attribute__((ext_vector_type(2)));
 typedef short short4v __attribute__((ext_vector_type(4)));
 
 namespace {
@@ -79,17 +82,44 @@ __device__ __forceinline__ floatx16 product(const Frag &a, const Frag &b, floatx
     return __builtin_amdgcn_mfma_f32_32x32x16_f16(a.lo, b.hi, c, 0, 0, 0);
 }
 
-// Eight values of a matrix kept in rows [sample][column], for sums over samples: lane l gets column `first` + l % 32 of samples
-// 8 (l / 32) .. + 7.  The transposing read gives a group of sixteen lanes four rows of sixteen columns, a column to each lane.
-__device__ __forceinline__ half8v read_columns(const _Float16 *m, int pitch, int first, int lane)
+// Pieces of FIT_ROWS samples: rows of N chunks of eight halves, where chunk c of row s lies at place c ^ turn(s).  LDS serves 256 bytes a cycle
+// from 64 banks; sixteen rows' reads of the same chunk, and the four rows by four chunks of a transposing read, then lie in different ones.
+// (Rows that were longer by 16 halves instead cost 51 of 141 million LDS cycles in conflicts.)
+// A lane's places differ by an exclusive or with a constant, so one of them is kept and the others are made as they are needed.
+template <int N>
+struct Rows {
+    _Float16 v[FIT_ROWS][N * 8];
+    static __device__ __forceinline__ int turn(int s)
+    {
+        if (N == 16) return (s & 3) << 2 | (s >> 2 & 3);
+        if (N == 8) return (s & 2) << 1 | (s >> 2 & 3);
+        return s >> 2 & 3;
+    }
+    // byte of chunk c of row s
+    static __device__ __forceinline__ int place(int s, int c) { return s * (N * 16) + ((c ^ turn(s)) << 4); }
+    __device__ __forceinline__ half8v &chunk(int place) { return *(half8v *)((char *)v + place); }
+    // For sums over samples: lane l gets column 32 t + l % 32 of samples 16 b + 8 (l / 32) .. + 7.  The transposing read gives a group
+    // of sixteen lanes four rows of sixteen columns, a column to each lane.  from: columns_from() of this lane.
+    static __device__ __forceinline__ int columns_from(int lane)
+    {
+        const int group = lane >> 4, i = lane & 15;
+        return place(8 * (group >> 1) + (i >> 2), 2 * (group & 1) + (i >> 1 & 1)) + 8 * (i & 1);
+    }
+    __device__ __forceinline__ half8v columns(int from, int b, int t) const
+    {
+        const auto read = [&](const int place) {
+            return __builtin_bit_cast(half4v, __builtin_amdgcn_ds_read_tr16_b64_v4i16((__attribute__((address_space(3))) short4v *)((const char *)v + place)));
+        };
+        const half4v p = read((from ^ t << 6) + b * 16 * N * 16), q = read((from ^ (t << 6 | 16)) + (b * 16 + 4) * N * 16);
+        return __builtin_shufflevector(p, q, 0, 1, 2, 3, 4, 5, 6, 7);
+    }
+};
+
+// Keeps the optimiser from computing everything that follows from a place before the loop, in registers there are not.
+__device__ __forceinline__ int afresh(int place)
 {
-    const int group = lane >> 4, i = lane & 15;
-    const _Float16 *p = m + (8 * (group >> 1) + (i >> 2)) * pitch + first + 16 * (group & 1) + 4 * (i & 3);
-    const auto read = [](const _Float16 *q) {
-        return __builtin_bit_cast(half4v, __builtin_amdgcn_ds_read_tr16_b64_v4i16((__attribute__((address_space(3))) short4v *)q));
-    };
-    const half4v a = read(p), b = read(p + 4 * pitch);
-    return __builtin_shufflevector(a, b, 0, 1, 2, 3, 4, 5, 6, 7);
+    asm volatile("" : "+v"(place));                         // no instruction
+    return place;
 }
 
 __device__ __forceinline__ float wave_max(float v)
@@ -108,34 +138,35 @@ __device__ __forceinline__ void meet()
     __builtin_amdgcn_fence(__ATOMIC_ACQUIRE, "workgroup", "local");
 }
 
-// Everything of a workgroup's that wavefronts share.  Rows of pieces are 16 halves longer than what they hold: eight words, so that
-// eight rows next to each other lie in different banks.
+// Everything of a workgroup's that wavefronts share.
 template <int H, int CT, bool GRAD>
 struct FitShared {
-    static constexpr int T = FIT_ROWS, UB = H / 32, KB = H / 16, HP = H + 16, XP = 32 * CT + 16;
+    static constexpr int T = FIT_ROWS, UB = H / 32, KB = H / 16, XN = CT == 3 ? 16 : 4 * CT;
+    // d1 of the samples before is kept for a stage longer where there is room for it
+    static constexpr int D1 = GRAD && (H == 64 || CT < 3) ? 2 : 1;
+    Rows<H / 8> d1[D1][2], dz2[GRAD ? 2 : 1], dz1[GRAD ? 2 : 1];    // [of which samples][piece]
+    Rows<XN> xs[2][2];                                      // [of which samples][piece]
     half8v w2t[GRAD ? UB : 1][GRAD ? KB : 1][2][64];        // W2^T as operands: [units of layer 1][of layer 2][piece][lane]
-    _Float16 d1[2][T][HP];                                  // [piece]
-    _Float16 xs[2][2][T][XP];                               // [of which samples][piece]
-    _Float16 dz2[GRAD ? 2 : 1][GRAD ? T : 1][HP], dz1[GRAD ? 2 : 1][GRAD ? T : 1][HP];
     float part[2][UB][T];                                   // output units: partial sums over 32 hidden units
-    float target[2][2][T], share[2][T], bad[2][2][T];       // bad: NaN where features are not finite
-    int real[2][T];
-    unsigned char keep[2][T][H / 8];                        // [layer]: which of eight units stay
+    float target[2][2][T], bad[2][2][T];                    // bad: NaN where features are not finite
+    float share[4][T];                                      // (of three tiles some wavefront may be at)
+    int real[2][T], pair[2][T];                             // pair: rows of the two sides that samples name, -1 both where they name none
+    unsigned char keep[2][2][T][H / 8];                     // [of which samples][layer]: which of eight units stay
     float b1[H], wsm[H], b2[H], w3[2][H];                   // by unit; b1, wsm and b2 with the scale and the dropout's factor of their layer
     float most[5][2 * UB];
 };
 
 // Layer 1 with the norm's weight and bias folded in, for the forward wavefronts' operands (or, wide, as rows of floats), with what its
-// bounds are made of; the last FIT_RANGE_PARTS workgroups find the largest target and, where nothing else bounds them, feature.
+// bounds are made of; the last `parts` workgroups find the largest target and, where nothing else bounds them, feature.
 struct FoldArgs {
     const float *W1, *b1, *g, *beta;
     int H, F, padded, half, wide;
     void *image;                                            // wide: [H][padded] floats; else fragments of pieces
     float *bias, *norm1, *norm2, *scale;                    // [H]; [1]
-    float *ranges;                                          // [2][FIT_RANGE_PARTS]: targets, features
+    float *ranges;                                          // [2][FIT_RANGE_PARTS]: targets, features; of each the first `parts`
     const float *target[2], *X[2];
     const int32_t *index[2];
-    int rows[2], features;                                  // features: 0 not wanted, 1 of all workloads, 2 of those the samples name
+    int rows[2], features, parts;                           // features: 0 not wanted, 1 of all workloads, 2 of those the samples name
     long long count;
 };
 
@@ -145,19 +176,23 @@ __global__ __launch_bounds__(256) void fold_kernel(FoldArgs a)
     if ((int)blockIdx.x >= rows) {
         __shared__ float most[2][4];
         const int part = blockIdx.x - rows;
-        const long long first = (long long)part * 256 + threadIdx.x, step = FIT_RANGE_PARTS * 256;
+        const long long first = (long long)part * 256 + threadIdx.x, step = (long long)a.parts * 256;
         float t = 0.0f, x = 0.0f;
-        for (int k = 0; k < 2; ++k)
-            if (a.target[k])
-                for (long long s = first; s < a.count; s += step) { const float v = fabsf(a.target[k][s]); if (v < INFINITY) t = fmaxf(t, v); }
+        const auto note = [](float &most, const float v) { const float u = fabsf(v); if (u < INFINITY) most = fmaxf(most, u); };
         for (int k = 0; k < 2; ++k) {
-            if (a.features == 1)
-                for (long long e = first; e < (long long)a.rows[k] * a.F; e += step) { const float v = fabsf(a.X[k][e]); if (v < INFINITY) x = fmaxf(x, v); }
+            if (a.target[k]) {
+#pragma unroll 8
+                for (long long s = first; s < a.count; s += step) note(t, a.target[k][s]);
+            }
+            if (a.features == 1) {
+                const long long all = (long long)a.rows[k] * a.F;
+#pragma unroll 8
+                for (long long e = first; e < all; e += step) note(x, a.X[k][e]);
+            }
             if (a.features == 2)
-                for (long long s = first; s < a.count; s += step) {
-                    const int i = a.index[k][s];
-                    if (i < 0 || i >= a.rows[k]) continue;
-                    for (int f = 0; f < a.F; ++f) { const float v = fabsf(a.X[k][(size_t)i * a.F + f]); if (v < INFINITY) x = fmaxf(x, v); }
+                for (long long e = first; e < a.count * a.F; e += step) {
+                    const int i = a.index[k][e / a.F];
+                    if (i >= 0 && i < a.rows[k]) note(x, a.X[k][(size_t)i * a.F + e % a.F]);
                 }
         }
         t = wave_max(t);
@@ -217,19 +252,20 @@ __global__ __launch_bounds__(256) void fold_kernel(FoldArgs a)
 
 // EXTRA: the predictor has the slowdown unit or the SM share (or both).
 template <int H, int CT, bool GRAD, bool EXTRA>
-__global__ __launch_bounds__(H * 4, 2) void fit_kernel(FitArgs a, const float *__restrict__ scale1, const float *__restrict__ norm1, const float *__restrict__ norm2,
-                                                       const float *__restrict__ ranges)
+__global__ __launch_bounds__(H * 4, 2) void fit_kernel(const FitArgs a, const float *__restrict__ scale1, const float *__restrict__ norm1, const float *__restrict__ norm2,
+                                                       const float *__restrict__ ranges, const int parts)
 {
     using L = FitShared<H, CT, GRAD>;
     using S = FitSums<H>;
-    constexpr int T = FIT_ROWS, UB = H / 32, KB = H / 16, XB = 2 * CT, HALF = 16 * CT, HP = L::HP, XP = L::XP;
+    constexpr int T = FIT_ROWS, UB = H / 32, KB = H / 16, XB = 2 * CT, HALF = 16 * CT;
     extern __shared__ __align__(16) char lds[];
     L &sh = *(L *)lds;
     const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), nn = lane & 31, hh = lane >> 5;
     const float minus_one = hidden_minus_one();
-    if (a.step) { const unsigned long long s = *a.step; a.rule.s0 = (unsigned)s; a.rule.s1 = (unsigned)(s >> 32); }
+    DropRule rule = a.rule;
+    if (a.step) { const unsigned long long s = *a.step; rule.s0 = (unsigned)s; rule.s1 = (unsigned)(s >> 32); }
     const bool slow = EXTRA && a.W3[1], with_share = EXTRA && a.W1sm;
-    const float factor = a.drop ? a.rule.factor : 1.0f;
+    const float factor = a.drop ? rule.factor : 1.0f;
     const long long tiles = (a.count + T - 1) / T;
     const int mine = (int)((tiles - blockIdx.x + gridDim.x - 1) / gridDim.x);
     const auto tile_of = [&](const int it) { return (long long)blockIdx.x + (long long)it * gridDim.x; };
@@ -252,7 +288,7 @@ __global__ __launch_bounds__(H * 4, 2) void fit_kernel(FitArgs a, const float *_
     }
     // largest of: targets, features, output weights of either unit, W2 and its columns' sums, z1
     float v[6] = {0.0f, 0.0f, 0.0f, 0.0f, largest, column};
-    if (tid < FIT_RANGE_PARTS) { v[0] = ranges[tid]; v[1] = ranges[FIT_RANGE_PARTS + tid]; }
+    if (tid < parts) { v[0] = ranges[tid]; v[1] = ranges[FIT_RANGE_PARTS + tid]; }
     if (tid < H) {
         v[2] = fabsf(a.W3[0][tid]);
         v[3] = slow ? fabsf(a.W3[1][tid]) : 0.0f;
@@ -328,41 +364,53 @@ __global__ __launch_bounds__(H * 4, 2) void fit_kernel(FitArgs a, const float *_
             __builtin_memcpy(v, __builtin_assume_aligned(a.W2 + unit * H + 16 * b + 8 * hh, 16), sizeof(v));
             w2[b] = as_operand(v);
         }
-        const float b3[2] = {*a.b3[0] + poison, slow ? *a.b3[1] + poison : 0.0f};
-        float gw3[16], gw3s[16], gb3[2] = {0.0f, 0.0f}, loss = 0.0f;
+        const float b3 = (EXTRA && slow && hh ? *a.b3[1] : *a.b3[0]) + poison;
+        float gw3[16], gw3s[16], gb3 = 0.0f, loss = 0.0f;
 #pragma unroll
         for (int k = 0; k < 16; ++k) gw3[k] = gw3s[k] = 0.0f;
-        const half8v *image = (const half8v *)a.W1 + (size_t)ub * XB * 2 * 64 + lane;
+        const int mine_at = Rows<H / 8>::place(nn, hh), features_at = Rows<L::XN>::place(nn, hh);
+        Frag w1[XB];
+#pragma unroll
+        for (int b = 0; b < XB; ++b) {
+            const half8v *image = (const half8v *)a.W1 + ((size_t)ub * XB + b) * 2 * 64 + lane;
+            w1[b] = Frag{image[0], image[64]};
+        }
         // eight values to a sample's row, as pieces
-        const auto put = [&](_Float16 *hi_to, _Float16 *lo_to, const float (&v)[8]) {
+        const auto put = [&](Rows<H / 8> *to, const int g, const float (&v)[8]) {
             _Float16 hi[8], lo[8];
             split(v, hi, lo, minus_one);
             half8v h, l;
 #pragma unroll
             for (int e = 0; e < 8; ++e) { h[e] = hi[e]; l[e] = lo[e]; }
-            *(half8v *)hi_to = h;
-            *(half8v *)lo_to = l;
+            const int place = afresh(mine_at) ^ (ub << 6 | g << 5);
+            to[0].chunk(place) = h;
+            to[1].chunk(place) = l;
         };
+        // columns 16 b + 8 hh .. + 7 of this lane's sample
+        const auto operand = [&](auto *rows, const int place, const int b) { return Frag{rows[0].chunk(place ^ b << 5), rows[1].chunk(place ^ b << 5)}; };
         // a unit's value after ReLU and dropout: its bit, as a mask
         const auto kept = [](const float z, const unsigned keep, const int e) {
-            return __uint_as_float(__float_as_uint(fmaxf(z, 0.0f)) & (unsigned)((int)(keep << (31 - e)) >> 31));
+            const int bit = e >> 1 | (e & 1) << 2;
+            return __uint_as_float(__float_as_uint(fmaxf(z, 0.0f)) & (unsigned)((int)(keep << (31 - bit)) >> 31));
         };
         const floatx16 zero = {0};
-        meet();                                             // the first samples are there
+        for (int k = 0; k < 4; ++k) meet();                 // the first samples are there
         for (int it = 0; it < mine; ++it) {
             const int now = it & 1;
             floatx16 z;
             bool open1[16];
+            {
+                const int features_here = afresh(features_at);
+                Frag x[XB];
 #pragma unroll
-            for (int b = 0; b < XB; ++b) {
-                const Frag w = {image[(2 * b) * 64], image[(2 * b + 1) * 64]};
-                const Frag x = {*(const half8v *)&sh.xs[now][0][nn][16 * b + 8 * hh], *(const half8v *)&sh.xs[now][1][nn][16 * b + 8 * hh]};
-                z = product(w, x, b == 0 ? zero : z);
+                for (int b = 0; b < XB; ++b) x[b] = operand(sh.xs[now], features_here, b);
+#pragma unroll
+                for (int b = 0; b < XB; ++b) z = product(w1[b], x[b], b == 0 ? zero : z);
             }
-            const float share = with_share ? sh.share[now][nn] : 0.0f;
+            const float share = with_share ? sh.share[it & 3][nn] : 0.0f;
 #pragma unroll
             for (int g = 0; g < 2; ++g) {
-                const unsigned keep = a.drop ? sh.keep[0][nn][4 * ub + hh + 2 * g] : 255u;
+                const unsigned keep = a.drop ? sh.keep[now][0][nn][4 * ub + hh + 2 * g] : 255u;
                 float v[8];
 #pragma unroll
                 for (int e = 0; e < 8; ++e) {
@@ -372,18 +420,19 @@ __global__ __launch_bounds__(H * 4, 2) void fit_kernel(FitArgs a, const float *_
                     v[e] = kept(h, keep, e);
                     open1[8 * g + e] = v[e] > 0.0f;
                 }
-                put(&sh.d1[0][nn][u0 + 16 * g], &sh.d1[1][nn][u0 + 16 * g], v);
+                put(sh.d1[L::D1 > 1 ? now : 0], g, v);
             }
             meet();
+            int here = afresh(mine_at);
 #pragma unroll
             for (int b = 0; b < KB; ++b) {
-                const Frag x = {*(const half8v *)&sh.d1[0][nn][16 * b + 8 * hh], *(const half8v *)&sh.d1[1][nn][16 * b + 8 * hh]};
+                const Frag x = operand(sh.d1[L::D1 > 1 ? now : 0], here, b);
                 z = product(w2[b], x, b == 0 ? zero : z);
             }
             float h2[16], zp = 0.0f, zs = 0.0f;
 #pragma unroll
             for (int g = 0; g < 2; ++g) {
-                const unsigned keep = a.drop ? sh.keep[1][nn][4 * ub + hh + 2 * g] : 255u;
+                const unsigned keep = a.drop ? sh.keep[now][1][nn][4 * ub + hh + 2 * g] : 255u;
 #pragma unroll
                 for (int e = 0; e < 8; ++e) {
                     const int k = u0 + 16 * g + e;
@@ -398,21 +447,23 @@ __global__ __launch_bounds__(H * 4, 2) void fit_kernel(FitArgs a, const float *_
             if (hh == 0) { sh.part[0][ub][nn] = zp; if (EXTRA) sh.part[1][ub][nn] = zs; }
             meet();
             const long long sample = tile_of(it) * T + nn;
-            const bool real = sh.real[now][nn], speaks = ub == 0 && hh == 0;
-            const float bad = sh.bad[now][0][nn] + sh.bad[now][1][nn];
-            float dz[2] = {0.0f, 0.0f};
+            const bool real = sh.real[now][nn], speaks = ub == 0 && (hh == 0 || slow);
+            // (with two output units either half of the wavefront takes one)
+            const int unit3 = EXTRA && slow ? hh : 0;
+            float z3 = b3 + sh.bad[now][0][nn] + sh.bad[now][1][nn];
 #pragma unroll
-            for (int q = 0; q < (EXTRA ? 2 : 1); ++q) {
-                if (q == 1 && !slow) break;
-                float zq = b3[q] + bad;
-#pragma unroll
-                for (int k = 0; k < UB; ++k) zq += sh.part[q][k][nn];
-                const float y = 1.0f / (1.0f + expf(-zq));
-                if (speaks && a.sigma[q] && sample < a.count) a.sigma[q][sample] = real ? y : 0.0f;
-                // what nobody has measured (a NaN) has no part in the loss
-                const float t = sh.target[now][q][nn], miss = t == t ? y - t : 0.0f;
-                dz[q] = t == t ? 2.0f * miss * y * (1.0f - y) : 0.0f;
-                if (speaks) { loss = fmaf(miss, miss, loss); gb3[q] += dz[q]; }
+            for (int k = 0; k < UB; ++k) z3 += sh.part[unit3][k][nn];
+            const float y = 1.0f / (1.0f + expf(-z3));
+            float *const sigma = EXTRA && unit3 ? a.sigma[1] : a.sigma[0];
+            if (speaks && sigma && sample < a.count) sigma[sample] = real ? y : 0.0f;
+            // what nobody has measured (a NaN) has no part in the loss
+            const float t = sh.target[now][unit3][nn], miss = t == t ? y - t : 0.0f, dz3 = t == t ? 2.0f * miss * y * (1.0f - y) : 0.0f;
+            if (speaks) { loss = fmaf(miss, miss, loss); gb3 += dz3; }
+            float dz[2] = {dz3, 0.0f};
+            if (EXTRA && slow) {
+                const auto s = __builtin_amdgcn_permlane32_swap(__float_as_uint(dz3), __float_as_uint(dz3), false, false);
+                dz[0] = __uint_as_float(s[0]);
+                dz[1] = __uint_as_float(s[1]);
             }
             if (!GRAD) continue;
             const float c0 = dz[0] * by_dz, c1 = dz[1] * by_dz;
@@ -430,13 +481,14 @@ __global__ __launch_bounds__(H * 4, 2) void fit_kernel(FitArgs a, const float *_
                     }
                     d[e] = h2[r] > 0.0f ? v : 0.0f;
                 }
-                put(&sh.dz2[0][nn][u0 + 16 * g], &sh.dz2[1][nn][u0 + 16 * g], d);
+                put(sh.dz2, g, d);
             }
             meet();
+            here = afresh(mine_at);
 #pragma unroll
             for (int b = 0; b < KB; ++b) {
                 const Frag w = {sh.w2t[ub][b][0][lane], sh.w2t[ub][b][1][lane]};
-                const Frag x = {*(const half8v *)&sh.dz2[0][nn][16 * b + 8 * hh], *(const half8v *)&sh.dz2[1][nn][16 * b + 8 * hh]};
+                const Frag x = operand(sh.dz2, here, b);
                 z = product(w, x, b == 0 ? zero : z);
             }
 #pragma unroll
@@ -444,7 +496,7 @@ __global__ __launch_bounds__(H * 4, 2) void fit_kernel(FitArgs a, const float *_
                 float d[8];
 #pragma unroll
                 for (int e = 0; e < 8; ++e) d[e] = open1[8 * g + e] ? z[8 * g + e] * by_d1 : 0.0f;
-                put(&sh.dz1[0][nn][u0 + 16 * g], &sh.dz1[1][nn][u0 + 16 * g], d);
+                put(sh.dz1, g, d);
             }
             meet();
         }
@@ -457,60 +509,79 @@ __global__ __launch_bounds__(H * 4, 2) void fit_kernel(FitArgs a, const float *_
             }
         }
         if (ub == 0) {
-            const float v[3] = {group_sum<64>(gb3[0]), group_sum<64>(gb3[1]), group_sum<64>(loss)};
-            if (lane == 0)
-#pragma unroll
-                for (int q = 0; q < 3; ++q) out[S::REST + q] = v[q];
+            // (without the slowdown unit the upper half has no part in them)
+            gb3 = group_sum<32>(gb3);
+            loss = group_sum<64>(loss);
+            if (nn == 0) out[S::REST + (hh == 0 ? REST_B3 : REST_B3S)] = gb3;
+            if (lane == 0) out[S::REST + REST_LOSS] = loss;
         }
         return;
     }
 
-    // ---- sums, and what is to come.  UB neighbouring lanes take the features of one side of a sample, EACH of them each.
+    // ---- sums, and what is to come.  UB neighbouring lanes take the features of one side of a sample, EACH of them each; the first of these
+    // wavefronts ("scout") looks up what the samples name and what was measured of them, a side to either half of it.
     constexpr int EACH = HALF / UB;
     const int place = tid - 64 * UB, row = place / UB, sub = place % UB, own = row >> 1, side = row & 1;
-    float x[EACH], next_target[2] = {0.0f, 0.0f}, next_share = 0.0f;
-    int ahead[2] = {-1, -1};                                // the pair that this lane's sample of the tile after the next names
+    const bool scout = ub == 0;
+    const float *const features = side ? a.X[1] : a.X[0];
+    const int all_features = (side ? a.rows[1] : a.rows[0]) > 0 ? (side ? a.rows[1] : a.rows[0]) * a.F : a.F;       // (at most 2^20 x 48)
+    float4v x[EACH / 4];
     bool next_real = false;
-    const auto look = [&](const int it) {                   // at indices
-        ahead[0] = ahead[1] = -1;
-        const long long s = tile_of(it) * T + own;
-        if (it < mine && s < a.count) { ahead[0] = a.index[0][s]; ahead[1] = a.index[1][s]; }
+    // (the scout's: loads without a condition, from a place that is there anyway, so that nothing waits for them before they are needed)
+    const int32_t *const index = hh ? a.index[1] : a.index[0];
+    const float *const targets = hh ? a.target[1] : a.target[0], *const shares = hh ? a.X[1] : a.X[0];
+    const int share_feature = hh ? a.sm_feature[1] : a.sm_feature[0];
+    int looked = 0, named = -1;
+    float next_target = __builtin_nanf(""), next_share = 0.0f;
+    const auto sample_of = [&](const int it) { const long long s = tile_of(it) * T + nn; return s < a.count ? s : a.count - 1; };
+    const auto look = [&](const int it) { looked = index[sample_of(it)]; };
+    const auto name = [&](const int it) {                   // what has been looked up: a sample that names no pair has no part in anything
+        const bool mine_real = tile_of(it) * T + nn < a.count && (unsigned)looked < (unsigned)(hh ? a.rows[1] : a.rows[0]);
+        const auto both = __builtin_amdgcn_permlane32_swap((unsigned)mine_real, (unsigned)mine_real, false, false);
+        named = (both[0] & both[1]) ? looked : -1;
+        sh.pair[hh][nn] = named;
     };
-    const auto fetch = [&](const int it) {                  // features and targets of the samples whose indices have been looked at
-        // a sample that names no pair has no part in anything
-        next_real = ahead[0] >= 0 && ahead[0] < a.rows[0] && ahead[1] >= 0 && ahead[1] < a.rows[1];
-        const long long s = tile_of(it) * T + own;
-#pragma unroll
-        for (int e = 0; e < EACH; ++e) x[e] = 0.0f;
-        if (next_real) {
-            const float *from = a.X[side] + (size_t)ahead[side] * a.F + sub * EACH;
-            if ((sub + 1) * EACH <= a.F) {
-                __builtin_memcpy(x, from, sizeof(x));
-            } else {
-#pragma unroll
-                for (int e = 0; e < EACH; ++e) if (sub * EACH + e < a.F) x[e] = from[e];
-            }
+    const auto ask = [&](const int it) {                    // what was measured, and the SM share, of the samples named last
+        if (targets) next_target = targets[sample_of(it)];
+        if (with_share) next_share = shares[(named < 0 ? 0 : named) * a.F + share_feature];
+    };
+    const auto answer = [&](const int it) {
+        const int to = it & 1;
+        sh.target[to][hh][nn] = named < 0 ? __builtin_nanf("") : next_target;
+        if (with_share) {
+            const auto both = __builtin_amdgcn_permlane32_swap(__float_as_uint(next_share), __float_as_uint(next_share), false, false);
+            const float share = fminf(1.0f - __uint_as_float(both[0]), __uint_as_float(both[1]));
+            if (hh == 0) sh.share[it & 3][nn] = named < 0 ? 0.0f : share;
         }
-        if (sub == 0 && side == 0) {
-            const float none = __builtin_nanf("");
-            next_target[0] = next_real && a.target[0] ? a.target[0][s] : none;
-            next_target[1] = next_real && a.target[1] ? a.target[1][s] : none;
-            if (with_share)
-                next_share = next_real ? fminf(1.0f - a.X[0][(size_t)ahead[0] * a.F + a.sm_feature[0]], a.X[1][(size_t)ahead[1] * a.F + a.sm_feature[1]]) : 0.0f;
+        if (hh == 0) sh.real[to][nn] = named >= 0;
+    };
+    const auto fetch = [&](const int part) {                // features of the samples named last, in two parts
+        const int at = sh.pair[side][own];
+        if (part == 0) next_real = at >= 0;
+        // (what a lane reads beyond its row is the next row's, and is left out when it is put to use; beyond the last row it reads nothing)
+        const int at_feature = (at < 0 ? 0 : at) * a.F + sub * EACH;
+#pragma unroll
+        for (int e = 0; e < EACH / 4; ++e) {
+            if (e % 2 != part) continue;
+            const int first = at_feature + 4 * e;
+            if (first + 4 <= all_features) x[e] = *(const float4v *)(features + first);
+            else
+#pragma unroll
+                for (int k = 0; k < 4; ++k) x[e][k] = features[first + k < all_features ? first + k : all_features - 1];
         }
     };
     const auto stage = [&](const int it) {                  // what has been fetched, normalised, as pieces
         const int to = it & 1;
         float sum = 0.0f, mean = 0.0f, by = s_x;
 #pragma unroll
-        for (int e = 0; e < EACH; ++e) sum += x[e];
+        for (int e = 0; e < EACH; ++e) sum += sub * EACH + e < a.F ? x[e / 4][e % 4] : 0.0f;
         sum = group_sum<UB>(sum);
         if (a.norm) {
             float squares = 0.0f;
             mean = sum / (float)a.F;
 #pragma unroll
             for (int e = 0; e < EACH; ++e) {
-                const float d = sub * EACH + e < a.F ? x[e] - mean : 0.0f;
+                const float d = sub * EACH + e < a.F ? x[e / 4][e % 4] - mean : 0.0f;
                 squares = fmaf(d, d, squares);
             }
             by = s_x / sqrtf(group_sum<UB>(squares) / (float)a.F + a.eps);
@@ -518,39 +589,56 @@ __global__ __launch_bounds__(H * 4, 2) void fit_kernel(FitArgs a, const float *_
         float v[EACH];
         _Float16 hi[EACH], lo[EACH];
 #pragma unroll
-        for (int e = 0; e < EACH; ++e) v[e] = sub * EACH + e < a.F && next_real ? (x[e] - mean) * by : 0.0f;
+        for (int e = 0; e < EACH; ++e) v[e] = sub * EACH + e < a.F && next_real ? (x[e / 4][e % 4] - mean) * by : 0.0f;
         split(v, hi, lo, minus_one);
 #pragma unroll
         for (int e = 0; e < EACH; e += 4) {
-            *(half4v *)&sh.xs[to][0][own][side * HALF + sub * EACH + e] = half4v{hi[e], hi[e + 1], hi[e + 2], hi[e + 3]};
-            *(half4v *)&sh.xs[to][1][own][side * HALF + sub * EACH + e] = half4v{lo[e], lo[e + 1], lo[e + 2], lo[e + 3]};
+            const int c = side * HALF + sub * EACH + e;
+            const int place = Rows<L::XN>::place(own, c >> 3) + 2 * (c & 4);
+            *(half4v *)((char *)&sh.xs[to][0] + place) = half4v{hi[e], hi[e + 1], hi[e + 2], hi[e + 3]};
+            *(half4v *)((char *)&sh.xs[to][1] + place) = half4v{lo[e], lo[e + 1], lo[e + 2], lo[e + 3]};
         }
-        if (sub == 0) {
-            sh.bad[to][side][own] = next_real ? sum * 0.0f : 0.0f;
-            if (side == 0) {
-                sh.target[to][0][own] = next_target[0];
-                sh.target[to][1][own] = next_target[1];
-                sh.share[to][own] = next_share;
-                sh.real[to][own] = next_real;
-            }
-        }
+        if (sub == 0) sh.bad[to][side][own] = next_real ? sum * 0.0f : 0.0f;
     };
-    const auto draw = [&](const int it, const int layer) {  // random bits
+    const unsigned short limit = (unsigned short)(rule.limit - 1);      // (a dropout's limit is at least 1)
+    const ushort2v below = {limit, limit};
+    const auto draw = [&](const int it, const int which) {  // random bits: of four groups of eight units that are this lane's, two a layer, one
+        const int layer = which >> 1, at = place + (which & 1) * 64 * UB, s = at / (H / 8), k = at % (H / 8);
+        // (groups of a tile share the upper word of their counter, and so half of the first two rounds is the same for all lanes)
+        const unsigned long long first = (unsigned long long)tile_of(it) * (T * (H / 8));
+        const Words4 bits = philox((unsigned)first + at, (unsigned)(first >> 32) | layer << 16, rule.s0, rule.s1, rule.k0, rule.k1);
+        // two halves at a time: 1 where a half is at least the limit.  Element 2 w + h ends as bit w + 4 h.
+        unsigned keep = 0;
 #pragma unroll
-        for (int q = 0; q < T * (H / 8) / (64 * UB); ++q) {
-            const int at = place + q * 64 * UB, s = at / (H / 8), k = at % (H / 8);
-            const Words4 bits = drop_bits(a.rule, (unsigned long long)(tile_of(it) * T + s) * (H / 8) + k, layer);
-            unsigned keep = 0;
-#pragma unroll
-            for (int e = 0; e < 8; ++e) keep |= drop_keeps(a.rule, bits, e) ? 1u << e : 0u;
-            sh.keep[layer][s][k] = (unsigned char)keep;
+        for (int w = 0; w < 4; ++w) {
+            const ushort2v above = __builtin_elementwise_min(__builtin_elementwise_sub_sat(__builtin_bit_cast(ushort2v, bits.w[w]), below), ushort2v{1, 1});
+            keep |= __builtin_bit_cast(unsigned, above) << w;
         }
+        sh.keep[it & 1][layer][s][k] = (unsigned char)(keep | keep >> 12);
     };
-    look(0);
+    static_assert(T * (H / 8) == 2 * 64 * UB, "groups");
+    if (scout) {
+        look(0);
+        const int first = looked;
+        look(1);
+        const int second = looked;
+        looked = first;
+        name(0);
+        ask(0);
+        looked = second;
+    }
+    meet();
     fetch(0);
+    fetch(1);
     stage(0);
-    look(1);
-    if (a.drop) { draw(0, 0); draw(0, 1); }
+    if (scout) answer(0);
+    meet();
+    if (scout) name(1);
+    meet();
+    fetch(0);
+    fetch(1);
+    if (scout) look(2);
+    if (a.drop) for (int q = 0; q < 4; ++q) draw(0, q);
     floatx16 gw2[GRAD ? UB : 1], gw1[GRAD ? CT : 1];
     float gb1 = 0.0f, gb2 = 0.0f, gsm = 0.0f, one = 1.0f;
     asm volatile("" : "+s"(one));                           // no instruction (see split)
@@ -563,51 +651,97 @@ __global__ __launch_bounds__(H * 4, 2) void fit_kernel(FitArgs a, const float *_
             for (int t = 0; t < CT; ++t) gw1[t][e] = 0.0f;
         }
     }
-    const auto columns_of = [&](const _Float16 *hi, const _Float16 *lo, const int pitch, const int first) {
-        return Frag{read_columns(hi, pitch, first, lane), read_columns(lo, pitch, first, lane)};
+    const int units_from = Rows<H / 8>::columns_from(lane), features_from = Rows<L::XN>::columns_from(lane);
+    const auto columns_of = [&](const auto *rows, const int from, const int b, const int t) { return Frag{rows[0].columns(from, b, t), rows[1].columns(from, b, t)}; };
+    // products of one operand with several, of which consecutive instructions never need one another's result
+    const auto products = [&](const Frag &d, const auto &with, floatx16 *sums) {
+        constexpr int N = sizeof(with) / sizeof(Frag);
+#pragma unroll
+        for (int t = 0; t < N; ++t) sums[t] = __builtin_amdgcn_mfma_f32_32x32x16_f16(d.hi, with[t].hi, sums[t], 0, 0, 0);
+#pragma unroll
+        for (int t = 0; t < N; ++t) sums[t] = __builtin_amdgcn_mfma_f32_32x32x16_f16(d.hi, with[t].lo, sums[t], 0, 0, 0);
+#pragma unroll
+        for (int t = 0; t < N; ++t) sums[t] = __builtin_amdgcn_mfma_f32_32x32x16_f16(d.lo, with[t].hi, sums[t], 0, 0, 0);
     };
-    const auto add_w1 = [&](const int of) {
+    // (meanwhile: work that needs none of the operands, while they are on their way)
+    const auto add_w1 = [&](const int it, const auto &meanwhile) {
+        const int of = it & 1;
+        Frag d[2], u[2][CT];
+        const int units = afresh(units_from), features = afresh(features_from);
+        const auto read = [&](const int b) {
+            d[b] = columns_of(sh.dz1, units, b, ub);
+#pragma unroll
+            for (int t = 0; t < CT; ++t) u[b][t] = columns_of(sh.xs[of], features, b, t);
+        };
+        read(0);
+        __builtin_amdgcn_sched_barrier(0);
+        meanwhile();
+        __builtin_amdgcn_sched_barrier(0);
+        read(1);
 #pragma unroll
         for (int b = 0; b < 2; ++b) {
-            const Frag d = columns_of(&sh.dz1[0][16 * b][0], &sh.dz1[1][16 * b][0], HP, 32 * ub);
+            products(d[b], u[b], gw1);
 #pragma unroll
-            for (int t = 0; t < CT; ++t) gw1[t] = product(d, columns_of(&sh.xs[of][0][16 * b][0], &sh.xs[of][1][16 * b][0], XP, 32 * t), gw1[t]);
-#pragma unroll
-            for (int e = 0; e < 8; ++e) gb1 = __builtin_fmaf((float)d.hi[e], one, __builtin_fmaf((float)d.lo[e], one, gb1));
+            for (int e = 0; e < 8; ++e) gb1 = __builtin_fmaf((float)d[b].hi[e], one, __builtin_fmaf((float)d[b].lo[e], one, gb1));
             if (EXTRA)
 #pragma unroll
                 for (int e = 0; e < 8; ++e) {
-                    const float by = sh.share[of][16 * b + 8 * hh + e];
-                    gsm = __builtin_fmaf((float)d.hi[e], by, __builtin_fmaf((float)d.lo[e], by, gsm));
+                    const float by = sh.share[it & 3][16 * b + 8 * hh + e];
+                    gsm = __builtin_fmaf((float)d[b].hi[e], by, __builtin_fmaf((float)d[b].lo[e], by, gsm));
                 }
         }
     };
+    const auto add_w2 = [&](const int of, const int b, const auto &meanwhile) {      // half of a tile's samples
+        const int units = afresh(units_from), of_d1 = L::D1 > 1 ? of : 0;
+        const Frag d = columns_of(sh.dz2, units, b, ub);
+        Frag u[2][UB / 2];
+        const auto read = [&](const int half) {
+#pragma unroll
+            for (int t = 0; t < UB / 2; ++t) u[half][t] = columns_of(sh.d1[of_d1], units, b, half * (UB / 2) + t);
+        };
+        read(0);
+        __builtin_amdgcn_sched_barrier(0);
+        meanwhile();
+        __builtin_amdgcn_sched_barrier(0);
+        read(1);
+        products(d, u[0], gw2);
+        products(d, u[1], gw2 + UB / 2);
+#pragma unroll
+        for (int e = 0; e < 8; ++e) gb2 = __builtin_fmaf((float)d.hi[e], one, __builtin_fmaf((float)d.lo[e], one, gb2));
+    };
     meet();
     for (int it = 0; it < mine; ++it) {
-        const bool more = it + 1 < mine;
-        if (more) { fetch(it + 1); look(it + 2); }
-        if (GRAD && it > 0) add_w1((it + 1) & 1);
+        const bool more = it + 1 < mine, drawn = more && a.drop;
+        const int now = it & 1, before = now ^ 1;
+        if (scout && more) ask(it + 1);
+        const auto draw_next = [&](const int which) { return [&, which]() { if (drawn) draw(it + 1, which); }; };
+        if (L::D1 > 1 && it > 0) add_w2(before, 1, [] {});
+        draw_next(0)();
         meet();
-        if (more) {
-            stage(it + 1);
-            if (a.drop) draw(it + 1, 0);
+        if (scout && more) answer(it + 1);
+        if (scout && it + 2 < mine) name(it + 2);
+        if (GRAD && it > 0) add_w1(it - 1, [] {});
+        draw_next(1)();
+        meet();
+        draw_next(2)();
+        if (more) stage(it + 1);
+        if (it + 2 < mine) fetch(0);
+        if (!GRAD) {
+            draw_next(3)();
+            if (it + 2 < mine) fetch(1);
+            if (scout) look(it + 3);
+            continue;
         }
         meet();
-        if (more && a.drop) draw(it + 1, 1);
-        if (!GRAD) continue;
-        meet();
-#pragma unroll
-        for (int b = 0; b < 2; ++b) {
-            const Frag d = columns_of(&sh.dz2[0][16 * b][0], &sh.dz2[1][16 * b][0], HP, 32 * ub);
-#pragma unroll
-            for (int t = 0; t < UB; ++t) gw2[t] = product(d, columns_of(&sh.d1[0][16 * b][0], &sh.d1[1][16 * b][0], HP, 32 * t), gw2[t]);
-#pragma unroll
-            for (int e = 0; e < 8; ++e) gb2 = __builtin_fmaf((float)d.hi[e], one, __builtin_fmaf((float)d.lo[e], one, gb2));
-        }
+        if (it + 2 < mine) fetch(1);
+        if (scout) look(it + 3);
+        add_w2(now, 0, draw_next(3));
+        if (L::D1 == 1) add_w2(now, 1, [] {});
         meet();
     }
     if (!GRAD || !out) return;
-    add_w1((mine + 1) & 1);
+    if (L::D1 > 1) add_w2((mine + 1) & 1, 1, [] {});
+    add_w1(mine - 1, [] {});
     const float by2 = 1.0f / (s_dz2 * s_d1), by1 = 1.0f / (s_dz1 * s_x);
 #pragma unroll
     for (int e = 0; e < 16; ++e) {
@@ -737,7 +871,7 @@ int launch_fit(mf_ctx *ctx, const FitArgs &a, const FitPlan &f)
         ctx->fit_configured |= flag;
     }
     hipLaunchKernelGGL((fit_kernel<H, CT, GRAD, EXTRA>), dim3(f.grid), dim3(H * 4), bytes, ctx->stream, a, ctx->fit_W1 + FOLD_SCALE, ctx->fit_W1 + FOLD_NORM1,
-                       ctx->fit_W1 + FOLD_NORM2, ctx->fit_W1 + FOLD_RANGES);
+                       ctx->fit_W1 + FOLD_NORM2, ctx->fit_W1 + FOLD_RANGES, f.parts);
     MF_HIP(hipGetLastError());
     return MF_OK;
 }
@@ -762,9 +896,9 @@ bool whole_floats(const void *p) { return ((uintptr_t)p & 3u) == 0; }
 int run_fit(mf_ctx *ctx, const mf_predictor *p, const float *d_on, int n, const float *d_off, int m, const mf_samples *s,
             const DropRule *rule, const uint64_t *d_step, float scale, const mf_gradients *g, float *d_loss, float *d_sigma, float *d_sigma_slow, void *d_work)
 {
-    const FitPlan f = fit_plan(ctx, p, s->count);
+    FitPlan f = fit_plan(ctx, p, s->count);
     FitArgs a{};
-    a.X[0] = d_on; a.X[1] = d_off;
+    a.X[0] = n > 0 ? d_on : ctx->fit_W1; a.X[1] = m > 0 ? d_off : ctx->fit_W1;      // (a row that can be read where there is none)
     a.rows[0] = n; a.rows[1] = m;
     a.F = p->F; a.columns = f.columns; a.padded = f.padded; a.half = f.half;
     a.index[0] = s->d_on; a.index[1] = s->d_off;
@@ -789,8 +923,16 @@ int run_fit(mf_ctx *ctx, const mf_predictor *p, const float *d_on, int n, const 
     w.norm1 = ctx->fit_W1 + FOLD_NORM1; w.norm2 = ctx->fit_W1 + FOLD_NORM2; w.ranges = ctx->fit_W1 + FOLD_RANGES;
     for (int k = 0; k < 2; ++k) { w.target[k] = a.target[k]; w.X[k] = a.X[k]; w.index[k] = a.index[k]; w.rows[k] = a.rows[k]; }
     w.count = a.count;
+    // (as many features are looked at as there are, or as the samples name, whichever is fewer)
     w.features = f.wide || (a.norm && !a.W1sm) ? 0 : 2 * s->count < (long long)n + m ? 2 : 1;
-    hipLaunchKernelGGL(fold_kernel, dim3(f.H / 4 + (f.wide ? 0 : FIT_RANGE_PARTS)), dim3(256), 0, ctx->stream, w);
+    if (!f.wide) {                                          // eight values a thread
+        long long values = (a.target[0] ? a.count : 0) + (a.target[1] ? a.count : 0);
+        if (w.features) values += p->F * (w.features == 2 ? 2 * a.count : (long long)n + m);
+        const long long parts = (values + 2047) / 2048;
+        f.parts = (int)(parts < 1 ? 1 : parts < FIT_RANGE_PARTS ? parts : FIT_RANGE_PARTS);
+    }
+    w.parts = f.parts;
+    hipLaunchKernelGGL(fold_kernel, dim3(f.H / 4 + f.parts), dim3(256), 0, ctx->stream, w);
     MF_HIP(hipGetLastError());
     const int rc = f.wide ? mf_launch_wide(ctx, a, f, g != nullptr) : f.H == 64 ? launch_fit_for<64>(ctx, a, f, g != nullptr) : launch_fit_for<128>(ctx, a, f, g != nullptr);
     if (rc != MF_OK || !a.partial) return rc;

@@ -8,7 +8,7 @@
 typedef float floatx16 __attribute__((ext_vector_type(16)));
 
 constexpr int FIT_WIDE_FROM = 49;                           // features a workload from which on fit_wide.hip takes over
-constexpr int FIT_RANGE_PARTS = 64;                         // workgroups that look for the largest target and feature
+constexpr int FIT_RANGE_PARTS = 256;                        // workgroups that look at most for the largest target and feature
 
 struct FitArgs {
     const float *X[2];
@@ -37,6 +37,7 @@ enum { REST_B3 = 0, REST_B3S, REST_LOSS };
 
 struct FitPlan {
     int H, columns, padded, half, passes, tiles, grid;      // tiles: of 32 columns that a pass over the samples keeps gradients of, for each wavefront
+    int parts;                                              // workgroups that look for bounds
     bool wide;
     int values(bool grad) const { return (H == 64 ? FitSums<64>::G : FitSums<128>::G) + (grad ? H * padded : 0); }
     long long step(bool grad) const { return (values(grad) + 15) & ~15; }

@@ -18,7 +18,7 @@ constexpr size_t wide_lds_bytes(bool grad)
 }
 
 template <int H, int GT, bool GRAD>
-__global__ __launch_bounds__(H * 4) void wide_kernel(FitArgs a)
+__global__ __launch_bounds__(H * 4) void wide_kernel(const FitArgs a)
 {
     constexpr int T = FIT_ROWS, PITCH = H + 4, XP = FIT_CHUNK + 4, UB = H / 32, THREADS = H * 4, QUADS = H / 8;
     using S = FitSums<H>;
@@ -31,7 +31,8 @@ __global__ __launch_bounds__(H * 4) void wide_kernel(FitArgs a)
     const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6, nn = lane & 31, hh = lane >> 5;
     const int ub = wave % UB, sh = wave / UB;               // units 32 ub .. and samples 32 sh .. of the forward pass are this wavefront's
     const int unit = 32 * ub + tile_unit(nn), mine = 32 * sh + nn, u0 = 32 * ub + 8 * hh;
-    if (a.step) { const unsigned long long s = *a.step; a.rule.s0 = (unsigned)s; a.rule.s1 = (unsigned)(s >> 32); }
+    DropRule rule = a.rule;
+    if (a.step) { const unsigned long long s = *a.step; rule.s0 = (unsigned)s; rule.s1 = (unsigned)(s >> 32); }
 
     for (int e = tid; e < H * H / 4; e += THREADS) *(float4 *)(w2 + e / (H / 4) * PITCH + e % (H / 4) * 4) = ((const float4 *)a.W2)[e];
     for (int e = tid; e < H; e += THREADS) {
@@ -42,7 +43,7 @@ __global__ __launch_bounds__(H * 4) void wide_kernel(FitArgs a)
         vec[4 * H + e] = a.W1sm ? a.W1sm[e] : 0.0f;
     }
     const float b3 = *a.b3[0], b3s = a.W3[1] ? *a.b3[1] : 0.0f;
-    const float factor = a.drop ? a.rule.factor : 1.0f;
+    const float factor = a.drop ? rule.factor : 1.0f;
     const int chunks = (a.padded + FIT_CHUNK - 1) / FIT_CHUNK;
     const int pass_chunk = blockIdx.y * GT;                 // this pass keeps gradients of layer 1 from this chunk on
 
@@ -65,7 +66,7 @@ __global__ __launch_bounds__(H * 4) void wide_kernel(FitArgs a)
             float v = 0.0f;
             if (c < a.columns && at_on[s] >= 0) {
                 const float2 m = moments[2 * s + side];
-                v = (a.X[side][(size_t)(side ? at_off[s] : at_on[s]) * a.F + c - (side ? a.F : 0)] - m.x) * m.y;
+                v = ((side ? a.X[1] : a.X[0])[(size_t)(side ? at_off[s] : at_on[s]) * a.F + c - (side ? a.F : 0)] - m.x) * m.y;
             }
             xs[s * XP + e % FIT_CHUNK] = v;
         }
@@ -75,13 +76,13 @@ __global__ __launch_bounds__(H * 4) void wide_kernel(FitArgs a)
 #pragma unroll
         for (int g = 0; g < 2; ++g) {
             Words4 bits;
-            if (a.drop) bits = drop_bits(a.rule, (unsigned long long)sample * (H / 8) + (u0 + 16 * g) / 8, layer);
+            if (a.drop) bits = drop_bits(rule, (unsigned long long)sample * (H / 8) + (u0 + 16 * g) / 8, layer);
 #pragma unroll
             for (int e = 0; e < 8; ++e) {
                 float v = z[8 * g + e] + bias[u0 + 16 * g + e];
                 if (layer == 0 && a.W1sm) v = fmaf(share_here, vec[4 * H + u0 + 16 * g + e], v);
                 v = relu(v);
-                if (a.drop) v = drop_keeps(a.rule, bits, e) ? v * factor : 0.0f;
+                if (a.drop) v = drop_keeps(rule, bits, e) ? v * factor : 0.0f;
                 h[8 * g + e] = v;
             }
         }
@@ -121,7 +122,7 @@ __global__ __launch_bounds__(H * 4) void wide_kernel(FitArgs a)
             const int at = side ? at_off[r >> 1] : at_on[r >> 1];
             float2 m = make_float2(0.0f, 1.0f);
             if (a.norm && at >= 0) {                        // (the lanes of a row agree)
-                const float *x = a.X[side] + (size_t)at * a.F;
+                const float *x = (side ? a.X[1] : a.X[0]) + (size_t)at * a.F;
                 float sum = 0.0f, squares = 0.0f;
                 for (int f = sub; f < a.F; f += EACH) sum += x[f];
                 m.x = group_sum<EACH>(sum) / (float)a.F;

@@ -291,9 +291,10 @@ struct DropArgs {
 // A thread takes the eight elements of a counter.  APART: rows lie apart in x or y, so an element's place needs its row;
 // eight elements that lie in one row are still loaded together.
 template <typename T, bool APART>
-__global__ __launch_bounds__(LAYER_THREADS) void dropout_kernel(DropArgs a)
+__global__ __launch_bounds__(LAYER_THREADS) void dropout_kernel(const DropArgs a)
 {
-    if (a.step) { const unsigned long long s = *a.step; a.rule.s0 = (unsigned)s; a.rule.s1 = (unsigned)(s >> 32); }
+    DropRule rule = a.rule;
+    if (a.step) { const unsigned long long s = *a.step; rule.s0 = (unsigned)s; rule.s1 = (unsigned)(s >> 32); }
     const int64_t groups = (a.total + 7) / 8;
     for (int64_t g = (int64_t)blockIdx.x * LAYER_THREADS + threadIdx.x; g < groups; g += (int64_t)gridDim.x * LAYER_THREADS) {
         const int64_t first = g * 8;
@@ -309,17 +310,17 @@ __global__ __launch_bounds__(LAYER_THREADS) void dropout_kernel(DropArgs a)
         const bool together = first + 8 <= a.total && (!APART || col + 8 <= a.width);
         float v[8];
         if (together) load_floats(v, x);
-        const Words4 bits = drop_bits(a.rule, (uint64_t)g, a.layer);
+        const Words4 bits = drop_bits(rule, (uint64_t)g, a.layer);
         if (together) {
 #pragma unroll
-            for (int t = 0; t < 8; ++t) v[t] = drop_keeps(a.rule, bits, t) ? v[t] * a.rule.factor : 0.0f;
+            for (int t = 0; t < 8; ++t) v[t] = drop_keeps(rule, bits, t) ? v[t] * rule.factor : 0.0f;
             store_floats(y, v);
         } else {
 #pragma unroll
             for (int t = 0; t < 8; ++t) {
                 if (first + t >= a.total) break;
                 const float u = (float)*x;
-                *y = (T)(drop_keeps(a.rule, bits, t) ? u * a.rule.factor : 0.0f);
+                *y = (T)(drop_keeps(rule, bits, t) ? u * rule.factor : 0.0f);
                 ++x; ++y;
                 if (APART && ++col == a.width) { col = 0; x += a.ldx - a.width; y += a.ldy - a.width; }
             }
