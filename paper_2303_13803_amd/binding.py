@@ -166,27 +166,37 @@ class Context:
             raise MuxmatchError(rc, detail)
         return rc
 
+    # (Every look at a tensor's attribute is a tenth of a microsecond or more, and the smallest calls are two on the device.)
     def _flat(self, t, dtype, count, what, optional=False):
         """Pointer of a contiguous tensor of `count` values on this context's device."""
         if t is None and optional:
             return None
-        if not isinstance(t, torch.Tensor) or not t.is_cuda or t.device.index != self.device or t.dtype != dtype or not t.is_contiguous():
+        if not isinstance(t, torch.Tensor) or t.get_device() != self.device or t.dtype != dtype or not t.is_contiguous():
             raise TypeError(f"{what}: expected a contiguous tensor of {dtype} on device {self.device}")
         if t.numel() != count:
             raise ValueError(f"{what}: expected {count} values, got {t.numel()}")
         return t.data_ptr() or None
 
-    def _rows(self, t, like, what):
-        """(pointer, pitch) of a matrix whose rows may lie apart but whose values lie side by side."""
-        if not isinstance(t, torch.Tensor) or not t.is_cuda or t.device.index != self.device or t.dtype not in LAYER_TYPES or t.dim() != 2:
-            raise TypeError(f"{what}: expected a float32, float16 or bfloat16 matrix on device {self.device}")
-        if like is not None and (t.dtype != like.dtype or t.shape != like.shape):
+    def _rows(self, t, kind, shape, what):
+        """(pointer, pitch) of a matrix of this type and shape whose rows may lie apart but whose values lie side by side."""
+        if not isinstance(t, torch.Tensor) or t.get_device() != self.device:
+            raise TypeError(f"{what}: expected a tensor on device {self.device}")
+        if t.dtype != kind or t.shape != shape:
             raise ValueError(f"{what}: expected a matrix of the input's shape and type")
-        rows, width = t.shape
-        pitch = t.stride(0) if rows > 1 else max(width, 1)
-        if (width > 1 and t.stride(1) != 1) or pitch < width:
+        pitch, step = t.stride()
+        rows, width = shape
+        if rows < 2:
+            pitch = max(width, 1)
+        if (step != 1 and width > 1) or pitch < width:
             raise ValueError(f"{what}: the values of a row have to lie side by side, rows must not overlap")
         return t.data_ptr() or None, pitch
+
+    def _matrix(self, t, what):
+        """Type, its number, and shape of a matrix."""
+        kind = t.dtype if isinstance(t, torch.Tensor) else None
+        if kind not in LAYER_TYPES or t.dim() != 2:
+            raise TypeError(f"{what}: expected a float32, float16 or bfloat16 matrix")
+        return kind, LAYER_TYPES[kind], t.shape
 
     def _work(self, work, needed):
         """The caller's scratch, or as much from torch's allocator, in the order of this context's stream."""
@@ -209,9 +219,11 @@ class Context:
 
     def layer_norm(self, x, weight, bias, y, eps=1e-5):
         """y = layer norm of the rows of x (float32, float16 or bfloat16; weight and bias float32).  y may be x."""
-        (px, ldx), (py, ldy) = self._rows(x, None, "x"), self._rows(y, x, "y")
-        rows, width = x.shape
-        self._check(_lib.mf_layer_norm(self._h, LAYER_TYPES[x.dtype], px, rows, width, ldx,
+        kind, number, shape = self._matrix(x, "x")
+        px, ldx = self._rows(x, kind, shape, "x")
+        py, ldy = self._rows(y, kind, shape, "y")
+        rows, width = shape
+        self._check(_lib.mf_layer_norm(self._h, number, px, rows, width, ldx,
                                        self._flat(weight, torch.float32, width, "weight"),
                                        self._flat(bias, torch.float32, width, "bias"), float(eps), py, ldy))
 
@@ -224,21 +236,26 @@ class Context:
 
     def layer_norm_grad(self, x, dy, weight, dx, dweight, dbias, eps=1e-5, work=None):
         """dx, dweight and dbias of layer_norm from dy.  dx may be x or dy."""
-        (px, ldx), (pdy, lddy), (pdx, lddx) = self._rows(x, None, "x"), self._rows(dy, x, "dy"), self._rows(dx, x, "dx")
-        rows, width = x.shape
+        kind, number, shape = self._matrix(x, "x")
+        px, ldx = self._rows(x, kind, shape, "x")
+        pdy, lddy = self._rows(dy, kind, shape, "dy")
+        pdx, lddx = self._rows(dx, kind, shape, "dx")
+        rows, width = shape
         work = self._work(work, _lib.mf_layer_norm_grad_work(self._h, rows, width))
         flat = lambda t, what: self._flat(t, torch.float32, width, what)
-        self._check(_lib.mf_layer_norm_grad(self._h, LAYER_TYPES[x.dtype], px, rows, width, ldx, pdy, lddy,
+        self._check(_lib.mf_layer_norm_grad(self._h, number, px, rows, width, ldx, pdy, lddy,
                                             flat(weight, "weight"), float(eps), pdx, lddx, flat(dweight, "dweight"),
                                             flat(dbias, "dbias"), work.data_ptr(), work.numel()))
 
     def dropout(self, x, y, p, seed, step=0, layer=0):
         """y = dropout of x, the mask made from (seed, step, layer, element); on a gradient, the backward pass.
         step: a number, or an int64 tensor of one value on the device.  y may be x."""
-        (px, ldx), (py, ldy) = self._rows(x, None, "x"), self._rows(y, x, "y")
+        kind, number, shape = self._matrix(x, "x")
+        px, ldx = self._rows(x, kind, shape, "x")
+        py, ldy = self._rows(y, kind, shape, "y")
         rule = self._dropout(p, seed, step)
-        self._check(_lib.mf_dropout(self._h, LAYER_TYPES[x.dtype], px, x.shape[0], x.shape[1], ldx, C.byref(rule),
-                                    int(layer), py, ldy))
+        rows, width = shape
+        self._check(_lib.mf_dropout(self._h, number, px, rows, width, ldx, C.byref(rule), int(layer), py, ldy))
 
     def _sides(self, pred, x_on, x_off):
         """Features of both sides: [n, F] and [m, F]."""

@@ -150,110 +150,69 @@ struct FitShared {
     float part[2][UB][T];                                   // output units: partial sums over 32 hidden units
     float target[2][2][T], bad[2][2][T];                    // bad: NaN where features are not finite
     float share[4][T];                                      // (of three tiles some wavefront may be at)
-    int real[2][T], pair[2][T];                             // pair: rows of the two sides that samples name, -1 both where they name none
+    int real[2][T], pair[2][2][T];                          // pair: rows of the two sides that samples name, -1 both where they name none
     unsigned char keep[2][2][T][H / 8];                     // [of which samples][layer]: which of eight units stay
     float b1[H], wsm[H], b2[H], w3[2][H];                   // by unit; b1, wsm and b2 with the scale and the dropout's factor of their layer
-    float most[5][2 * UB];
+    float most[10][2 * UB];
 };
 
-// Layer 1 with the norm's weight and bias folded in, for the forward wavefronts' operands (or, wide, as rows of floats), with what its
-// bounds are made of; the last `parts` workgroups find the largest target and, where nothing else bounds them, feature.
+// For predictors of many features (wide): layer 1 with the norm's weight and bias folded in, its rows padded with zeros, a wavefront for each
+// hidden unit.  Else the largest feature, where nothing else bounds those that a fit sees: of a predictor without a norm all of them, of one
+// with an SM share those it is made of; of all workloads or those that the samples name, whichever are fewer.
 struct FoldArgs {
     const float *W1, *b1, *g, *beta;
-    int H, F, padded, half, wide;
-    void *image;                                            // wide: [H][padded] floats; else fragments of pieces
-    float *bias, *norm1, *norm2, *scale;                    // [H]; [1]
-    float *ranges;                                          // [2][FIT_RANGE_PARTS]: targets, features; of each the first `parts`
-    const float *target[2], *X[2];
+    int F, padded, wide;
+    float *W, *bias, *ranges;                               // [H][padded], [H]; [parts]
+    const float *X[2];
     const int32_t *index[2];
-    int rows[2], features, parts;                           // features: 0 not wanted, 1 of all workloads, 2 of those the samples name
+    int rows[2], first[2], width, listed, parts;            // features first .. first + width of either side
     long long count;
 };
 
 __global__ __launch_bounds__(256) void fold_kernel(FoldArgs a)
 {
-    const int lane = threadIdx.x & 63, rows = a.H / 4;
-    if ((int)blockIdx.x >= rows) {
-        __shared__ float most[2][4];
-        const int part = blockIdx.x - rows;
-        const long long first = (long long)part * 256 + threadIdx.x, step = (long long)a.parts * 256;
-        float t = 0.0f, x = 0.0f;
-        const auto note = [](float &most, const float v) { const float u = fabsf(v); if (u < INFINITY) most = fmaxf(most, u); };
+    const int lane = threadIdx.x & 63;
+    if (!a.wide) {
+        __shared__ float most[4];
+        const long long first = (long long)blockIdx.x * 256 + threadIdx.x, step = (long long)a.parts * 256;
+        float x = 0.0f;
         for (int k = 0; k < 2; ++k) {
-            if (a.target[k]) {
+            const float *X = (k ? a.X[1] : a.X[0]) + (k ? a.first[1] : a.first[0]);
+            const int32_t *index = k ? a.index[1] : a.index[0];
+            const int rows = k ? a.rows[1] : a.rows[0];
+            const long long all = (a.listed ? a.count : rows) * a.width;
 #pragma unroll 8
-                for (long long s = first; s < a.count; s += step) note(t, a.target[k][s]);
+            for (long long e = first; e < all; e += step) {
+                int row = (int)(e / a.width);
+                if (a.listed) row = index[row];
+                if ((unsigned)row >= (unsigned)rows) continue;
+                const float v = fabsf(X[(size_t)row * a.F + (int)(e % a.width)]);
+                if (v < INFINITY) x = fmaxf(x, v);
             }
-            if (a.features == 1) {
-                const long long all = (long long)a.rows[k] * a.F;
-#pragma unroll 8
-                for (long long e = first; e < all; e += step) note(x, a.X[k][e]);
-            }
-            if (a.features == 2)
-                for (long long e = first; e < a.count * a.F; e += step) {
-                    const int i = a.index[k][e / a.F];
-                    if (i >= 0 && i < a.rows[k]) note(x, a.X[k][(size_t)i * a.F + e % a.F]);
-                }
         }
-        t = wave_max(t);
         x = wave_max(x);
-        if (lane == 0) { most[0][threadIdx.x >> 6] = t; most[1][threadIdx.x >> 6] = x; }
+        if (lane == 0) most[threadIdx.x >> 6] = x;
         __syncthreads();
-        if (threadIdx.x < 2) a.ranges[threadIdx.x * FIT_RANGE_PARTS + part] = fmaxf(fmaxf(most[threadIdx.x][0], most[threadIdx.x][1]), fmaxf(most[threadIdx.x][2], most[threadIdx.x][3]));
+        if (threadIdx.x == 0) a.ranges[blockIdx.x] = fmaxf(fmaxf(most[0], most[1]), fmaxf(most[2], most[3]));
         return;
     }
-    const auto folded = [&](const int k, const int c, float *times_beta) {
-        const int side = c >= a.half, f = c - side * a.half;
-        if (f >= a.F) return 0.0f;
-        const int at = side * a.F + f;
-        const float w = a.W1[(size_t)k * 2 * a.F + at];
-        if (times_beta) *times_beta = a.g ? w * a.beta[at] : 0.0f;
-        return a.g ? w * a.g[at] : w;
-    };
-    const int k = blockIdx.x * 4 + (threadIdx.x >> 6);
-    float sum = 0.0f, norm1 = 0.0f, norm2 = 0.0f;
+    const int k = blockIdx.x * 4 + (threadIdx.x >> 6), columns = 2 * a.F;
+    float sum = 0.0f;
     for (int c = lane; c < a.padded; c += 64) {
-        float more = 0.0f;
-        const float v = folded(k, c, &more);
-        sum += more;
-        norm1 += fabsf(v);
-        norm2 = fmaf(v, v, norm2);
-        if (a.wide) ((float *)a.image)[(size_t)k * a.padded + c] = v;
+        float v = 0.0f;
+        if (c < columns) {
+            v = a.W1[(size_t)k * columns + c];
+            if (a.g) { sum = fmaf(v, a.beta[c], sum); v *= a.g[c]; }
+        }
+        a.W[(size_t)k * a.padded + c] = v;
     }
     sum = group_sum<64>(sum);
-    norm1 = group_sum<64>(norm1);
-    norm2 = group_sum<64>(norm2);
-    if (lane == 0) {
-        a.bias[k] = a.b1[k] + sum;
-        a.norm1[k] = norm1;
-        a.norm2[k] = sqrtf(norm2);
-    }
-    if (a.wide) return;
-    // (every workgroup looks for the largest weight itself: no more than 48 KB, and no launch between)
-    __shared__ float most[4];
-    float largest = 0.0f;
-#pragma unroll 8
-    for (int e = threadIdx.x; e < a.H * 2 * a.F; e += 256) largest = fmaxf(largest, fabsf(a.g ? a.W1[e] * a.g[e % (2 * a.F)] : a.W1[e]));
-    largest = wave_max(largest);
-    if (lane == 0) most[threadIdx.x >> 6] = largest;
-    __syncthreads();
-    const float scale = scale_below(fmaxf(fmaxf(most[0], most[1]), fmaxf(most[2], most[3])));
-    if (blockIdx.x == 0 && threadIdx.x == 0) *a.scale = scale;
-    const int blocks = a.padded / 16, m = tile_unit(k & 31);
-    for (int c = lane; c < a.padded; c += 64) {
-        const float v[2] = {folded(k, c, nullptr) * scale, 0.0f};
-        _Float16 hi[2], lo[2];
-        split(v, hi, lo, -1.0f);
-        _Float16 *to = (_Float16 *)a.image + ((size_t)((k >> 5) * blocks + (c >> 4)) * 2 * 64 + ((c >> 3) & 1) * 32 + m) * 8 + (c & 7);
-        to[0] = hi[0];
-        to[64 * 8] = lo[0];
-    }
+    if (lane == 0) a.bias[k] = a.b1[k] + sum;
 }
 
 // EXTRA: the predictor has the slowdown unit or the SM share (or both).
 template <int H, int CT, bool GRAD, bool EXTRA>
-__global__ __launch_bounds__(H * 4, 2) void fit_kernel(const FitArgs a, const float *__restrict__ scale1, const float *__restrict__ norm1, const float *__restrict__ norm2,
-                                                       const float *__restrict__ ranges, const int parts)
+__global__ __launch_bounds__(H * 4, 2) void fit_kernel(const FitArgs a, const float *__restrict__ ranges, const int parts)
 {
     using L = FitShared<H, CT, GRAD>;
     using S = FitSums<H>;
@@ -272,74 +231,190 @@ __global__ __launch_bounds__(H * 4, 2) void fit_kernel(const FitArgs a, const fl
     const bool forward = wave < UB;
     const int ub = forward ? wave : wave - UB, unit = 32 * ub + tile_unit(nn), u0 = 32 * ub + 8 * hh;
 
-    // ---- bounds, and the scales that follow.  W2 and its transpose are read as the operands that the forward wavefronts make of them.
-    float w[KB][8], largest = 0.0f, column = 0.0f, poison = 0.0f;
+    // ---- what is to come, the business of the wavefronts that sum up: UB neighbouring lanes take the features of one side of a sample, EACH of them each; the first of these
+    // wavefronts ("scout") looks up what the samples name and what was measured of them, a side to either half of it.
+    constexpr int EACH = HALF / UB;
+    const int place = tid - 64 * UB, row = place / UB, sub = place % UB, own = row >> 1, side = row & 1;
+    const bool scout = ub == 0;
+    const float *const features = side ? a.X[1] : a.X[0];
+    const int all_features = (side ? a.rows[1] : a.rows[0]) > 0 ? (side ? a.rows[1] : a.rows[0]) * a.F : a.F;       // (at most 2^20 x 48)
+    float4v x[EACH / 4];
+    bool next_real = false;
+    // (the scout's: loads without a condition, from a place that is there anyway, so that nothing waits for them before they are needed)
+    const int32_t *const index = hh ? a.index[1] : a.index[0];
+    const float *const targets = hh ? a.target[1] : a.target[0], *const shares = hh ? a.X[1] : a.X[0];
+    const int share_feature = hh ? a.sm_feature[1] : a.sm_feature[0];
+    int looked = 0, looked_first = 0, named = -1;
+    float next_target = __builtin_nanf(""), next_share = 0.0f;
+    const auto sample_of = [&](const int it) { const long long s = tile_of(it) * T + nn; return s < a.count ? s : a.count - 1; };
+    const auto look = [&](const int it, int &to) { to = index[sample_of(it)]; };
+    const auto name = [&](const int it, const int looked) { // what has been looked up: a sample that names no pair has no part in anything
+        const bool mine_real = tile_of(it) * T + nn < a.count && (unsigned)looked < (unsigned)(hh ? a.rows[1] : a.rows[0]);
+        const auto both = __builtin_amdgcn_permlane32_swap((unsigned)mine_real, (unsigned)mine_real, false, false);
+        named = (both[0] & both[1]) ? looked : -1;
+        sh.pair[it & 1][hh][nn] = named;
+    };
+    const auto ask = [&](const int it) {                    // what was measured, and the SM share, of the samples named last
+        if (targets) next_target = targets[sample_of(it)];
+        if (with_share) next_share = shares[(named < 0 ? 0 : named) * a.F + share_feature];
+    };
+    const auto answer = [&](const int it) {
+        const int to = it & 1;
+        sh.target[to][hh][nn] = named < 0 ? __builtin_nanf("") : next_target;
+        if (with_share) {
+            const auto both = __builtin_amdgcn_permlane32_swap(__float_as_uint(next_share), __float_as_uint(next_share), false, false);
+            const float share = fminf(1.0f - __uint_as_float(both[0]), __uint_as_float(both[1]));
+            if (hh == 0) sh.share[it & 3][nn] = named < 0 ? 0.0f : share;
+        }
+        if (hh == 0) sh.real[to][nn] = named >= 0;
+    };
+    const auto fetch = [&](const int it, const int part) {  // features of the samples named, in two parts
+        const int at = sh.pair[it & 1][side][own];
+        if (part == 0) next_real = at >= 0;
+        // (what a lane reads beyond its row is the next row's, and is left out when it is put to use; beyond the last row it reads nothing)
+        const int at_feature = (at < 0 ? 0 : at) * a.F + sub * EACH;
+#pragma unroll
+        for (int e = 0; e < EACH / 4; ++e) {
+            if (e % 2 != part) continue;
+            const int first = at_feature + 4 * e;
+            if (first + 4 <= all_features) x[e] = *(const float4v *)(features + first);
+            else
+#pragma unroll
+                for (int k = 0; k < 4; ++k) x[e][k] = features[first + k < all_features ? first + k : all_features - 1];
+        }
+    };
+    if (!forward && scout) {                                // (on their way during all that follows)
+        look(0, looked_first);
+        look(1, looked);
+    }
+
+    // ---- bounds, and the scales that follow.  Weights are read as the operands that the forward wavefronts make of them: layer 1's with the
+    // norm's weight, W2's transpose (or, without a way back, W2), a unit's in two lanes.
+    float w[KB][8], u1[XB][8], bias1 = 0.0f, poison = 0.0f;
+    // largest of: targets, features, output weights of either unit, weights of layers 2 and 1, columns' sums of W2, z1 without features and for each
+    float v[9] = {0.0f, 0.0f, 0.0f, 0.0f, 0.0f, 0.0f, 0.0f, 0.0f, 0.0f};
+    const float length = sqrtf((float)a.F);
+    const auto read_w2 = [&](const int b, float (&to)[8]) {
+#pragma unroll
+        for (int e = 0; e < 8; e += 4) {
+            const float4 r = *(const float4 *)(a.W2 + unit * H + 16 * b + 8 * hh + e);
+            to[e] = r.x; to[e + 1] = r.y; to[e + 2] = r.z; to[e + 3] = r.w;
+        }
+    };
     if (forward) {
+#pragma unroll
+        for (int b = 0; b < KB; ++b) {
+            if (GRAD) {
+#pragma unroll
+                for (int e = 0; e < 8; ++e) w[b][e] = a.W2[(16 * b + 8 * hh + e) * H + unit];
+            } else {
+                read_w2(b, w[b]);
+            }
+        }
+        float more = 0.0f, sum = 0.0f, squares = 0.0f;
+#pragma unroll
+        for (int b = 0; b < XB; ++b) {
+            const int c = 16 * b + 8 * hh, of = c >= HALF, f = c - of * HALF;
+            float g[8], beta[8];
+            if (a.F % 8 == 0) {
+                const int at = f < a.F ? of * a.F + f : 0;
+#pragma unroll
+                for (int e = 0; e < 8; e += 4) {
+                    const float4v r = *(const float4v *)(a.W1 + (size_t)unit * 2 * a.F + at + e);
+                    const float4v rg = a.norm ? *(const float4v *)(a.g + at + e) : float4v{1.0f, 1.0f, 1.0f, 1.0f};
+                    const float4v rb = a.norm ? *(const float4v *)(a.beta + at + e) : float4v{0.0f, 0.0f, 0.0f, 0.0f};
+#pragma unroll
+                    for (int k = 0; k < 4; ++k) { u1[b][e + k] = r[k]; g[e + k] = rg[k]; beta[e + k] = rb[k]; }
+                }
+            } else {
+#pragma unroll
+                for (int e = 0; e < 8; ++e) {
+                    const int at = f + e < a.F ? of * a.F + f + e : 0;
+                    u1[b][e] = a.W1[(size_t)unit * 2 * a.F + at];
+                    g[e] = a.norm ? a.g[at] : 1.0f;
+                    beta[e] = a.norm ? a.beta[at] : 0.0f;
+                }
+            }
+#pragma unroll
+            for (int e = 0; e < 8; ++e) {
+                const bool there = f + e < a.F;
+                more += there ? u1[b][e] * beta[e] : 0.0f;
+                u1[b][e] = there ? u1[b][e] * g[e] : 0.0f;
+                v[5] = fmaxf(v[5], fabsf(u1[b][e]));
+                sum += fabsf(u1[b][e]);
+                squares = fmaf(u1[b][e], u1[b][e], squares);
+            }
+        }
+        sum = both_halves(sum);
+        bias1 = a.b1[unit] + both_halves(more);
+        const float w_share = with_share ? a.W1sm[unit] : 0.0f;
+        v[7] = fabsf(bias1) + fabsf(w_share) + (a.norm ? sqrtf(both_halves(squares)) * length * 1.42f : 0.0f);
+        v[8] = fabsf(w_share) + (a.norm ? 0.0f : sum);
+        float column = 0.0f;
 #pragma unroll
         for (int b = 0; b < KB; ++b)
 #pragma unroll
-            for (int e = 0; e < 8; ++e) {
-                w[b][e] = a.W2[(16 * b + 8 * hh + e) * H + unit];
-                largest = fmaxf(largest, fabsf(w[b][e]));
-                column += fabsf(w[b][e]);
-            }
-        column = both_halves(column);
-        poison = column * 0.0f;                             // NaN if one of them is not finite
+            for (int e = 0; e < 8; ++e) { v[4] = fmaxf(v[4], fabsf(w[b][e])); column += fabsf(w[b][e]); }
+        v[6] = both_halves(column);
+        poison = (v[6] + bias1 + sum + w_share) * 0.0f;     // NaN if one of them is not finite
     }
-    // largest of: targets, features, output weights of either unit, W2 and its columns' sums, z1
-    float v[6] = {0.0f, 0.0f, 0.0f, 0.0f, largest, column};
-    if (tid < parts) { v[0] = ranges[tid]; v[1] = ranges[FIT_RANGE_PARTS + tid]; }
     if (tid < H) {
         v[2] = fabsf(a.W3[0][tid]);
         v[3] = slow ? fabsf(a.W3[1][tid]) : 0.0f;
-        poison += (norm1[tid] + a.b1[tid] + a.b2[tid] + (with_share ? a.W1sm[tid] : 0.0f)) * 0.0f;
+        poison += a.b2[tid] * 0.0f;
     }
-    const auto most_of = [&](float (&v)[6]) {
-#pragma unroll
-        for (int q = 0; q < 6; ++q) v[q] = wave_max(v[q]);
-        for (int q = 0; q < 6; q += 5) {                    // five at a time
-            __syncthreads();
-#pragma unroll
-            for (int k = 0; k < 5; ++k) if (q + k < 6 && lane == 0) sh.most[k][wave] = v[q + k];
-            __syncthreads();
-#pragma unroll
-            for (int k = 0; k < 5; ++k)
-                if (q + k < 6)
-                    for (int x = 0; x < 2 * UB; ++x) v[q + k] = fmaxf(v[q + k], sh.most[k][x]);
+    if (tid < parts) v[1] = ranges[tid];
+    if (GRAD)                                               // this workgroup's own targets
+#pragma unroll 4
+        for (int it = tid / T; it < mine; it += H * 4 / T) {
+            const long long s = tile_of(it) * T + tid % T, at = s < a.count ? s : a.count - 1;
+            const float t = fabsf(a.target[0][at]), ts = slow ? fabsf(a.target[1][at]) : 0.0f;
+            if (t < INFINITY) v[0] = fmaxf(v[0], t);
+            if (ts < INFINITY) v[0] = fmaxf(v[0], ts);
         }
-    };
-    most_of(v);
-    const float most_x = v[1], length = sqrtf((float)a.F);
-    const float s_x = scale_below(a.norm ? length * 1.001f : most_x), s_w2 = scale_below(v[4]);
-    const float bound2 = 0.5f * (1.0f + v[0]) * (v[2] + v[3]) * factor * 1.001f;
-    const float s_dz2 = scale_below(bound2), s_dz1 = scale_below(bound2 * factor * v[5] * 1.001f);
-    float z1 = 0.0f;
-    if (tid < H) {
-        z1 = fabsf(a.b1[tid]) + (a.norm ? norm2[tid] * length * 1.42f : norm1[tid] * most_x);
-        if (with_share) z1 += fabsf(a.W1sm[tid]) * (1.0f + most_x);
+#pragma unroll
+    for (int q = 0; q < 9; ++q) {
+        v[q] = wave_max(v[q]);
+        if (lane == 0) sh.most[q][wave] = v[q];
     }
-    z1 = wave_max(z1);
     poison = group_sum<64>(poison);
-    __syncthreads();
-    if (lane == 0) { sh.most[0][wave] = z1; sh.most[1][wave] = poison; }
-    __syncthreads();
+    if (lane == 0) sh.most[9][wave] = poison;
+    int named_first = -1;
+    if (!forward && scout) {
+        name(0, looked_first);
+        named_first = named;
+        ask(0);
+        name(1, looked);
+    }
+    meet();
+    if (!forward) {
+        fetch(0, 0);
+        fetch(0, 1);
+    }
     poison = 0.0f;
-    for (int x = 0; x < 2 * UB; ++x) { z1 = fmaxf(z1, sh.most[0][x]); poison += sh.most[1][x]; }
-    const float s_d1 = scale_below(z1 * factor * 1.001f);
+    for (int x = 0; x < 2 * UB; ++x) {
+#pragma unroll
+        for (int q = 0; q < 9; ++q) v[q] = fmaxf(v[q], sh.most[q][x]);
+        poison += sh.most[9][x];
+    }
+    const float s_x = scale_below(a.norm ? length * 1.001f : v[1]), s_w2 = scale_below(v[4]), s_w1 = scale_below(v[5]);
+    const float bound2 = 0.5f * (1.0f + v[0]) * (v[2] + v[3]) * factor * 1.001f;
+    const float s_dz2 = scale_below(bound2), s_dz1 = scale_below(bound2 * factor * v[6] * 1.001f);
+    const float s_d1 = scale_below((v[7] + v[8] * v[1]) * factor * 1.001f);
     // what accumulators of the three products are multiplied with
-    const float by_z1 = factor * s_d1 / (s_x * *scale1), by_z2 = factor / (s_d1 * s_w2), by_d1 = factor * s_dz1 / (s_dz2 * s_w2), by_dz = factor * s_dz2;
+    const float by_z1 = factor * s_d1 / (s_x * s_w1), by_z2 = factor / (s_d1 * s_w2), by_d1 = factor * s_dz1 / (s_dz2 * s_w2), by_dz = factor * s_dz2;
     if (tid < H) {
-        sh.b1[tid] = a.b1[tid] * (factor * s_d1);
         sh.wsm[tid] = with_share ? a.W1sm[tid] * (factor * s_d1) : 0.0f;
         sh.b2[tid] = a.b2[tid] * factor;
         sh.w3[0][tid] = a.W3[0][tid];
         sh.w3[1][tid] = slow ? a.W3[1][tid] : 0.0f;
     }
-    const auto as_operand = [&](const float (&from)[8]) {
+    if (forward && hh == 0) sh.b1[unit] = bias1 * (factor * s_d1);
+    const auto as_operand = [&](const float (&from)[8], const float scale) {
         float v[8];
         _Float16 hi[8], lo[8];
 #pragma unroll
-        for (int e = 0; e < 8; ++e) v[e] = from[e] * s_w2;
+        for (int e = 0; e < 8; ++e) v[e] = from[e] * scale;
         split(v, hi, lo, minus_one);
         Frag f;
 #pragma unroll
@@ -352,7 +427,7 @@ __global__ __launch_bounds__(H * 4, 2) void fit_kernel(const FitArgs a, const fl
         if (GRAD) {
 #pragma unroll
             for (int b = 0; b < KB; ++b) {
-                const Frag f = as_operand(w[b]);
+                const Frag f = as_operand(w[b], s_w2);
                 sh.w2t[ub][b][0][lane] = f.hi;
                 sh.w2t[ub][b][1][lane] = f.lo;
             }
@@ -360,9 +435,8 @@ __global__ __launch_bounds__(H * 4, 2) void fit_kernel(const FitArgs a, const fl
         Frag w2[KB];
 #pragma unroll
         for (int b = 0; b < KB; ++b) {
-            float v[8];
-            __builtin_memcpy(v, __builtin_assume_aligned(a.W2 + unit * H + 16 * b + 8 * hh, 16), sizeof(v));
-            w2[b] = as_operand(v);
+            if (GRAD) read_w2(b, w[b]);
+            w2[b] = as_operand(w[b], s_w2);
         }
         const float b3 = (EXTRA && slow && hh ? *a.b3[1] : *a.b3[0]) + poison;
         float gw3[16], gw3s[16], gb3 = 0.0f, loss = 0.0f;
@@ -371,10 +445,7 @@ __global__ __launch_bounds__(H * 4, 2) void fit_kernel(const FitArgs a, const fl
         const int mine_at = Rows<H / 8>::place(nn, hh), features_at = Rows<L::XN>::place(nn, hh);
         Frag w1[XB];
 #pragma unroll
-        for (int b = 0; b < XB; ++b) {
-            const half8v *image = (const half8v *)a.W1 + ((size_t)ub * XB + b) * 2 * 64 + lane;
-            w1[b] = Frag{image[0], image[64]};
-        }
+        for (int b = 0; b < XB; ++b) w1[b] = as_operand(u1[b], s_w1);
         // eight values to a sample's row, as pieces
         const auto put = [&](Rows<H / 8> *to, const int g, const float (&v)[8]) {
             _Float16 hi[8], lo[8];
@@ -394,7 +465,7 @@ __global__ __launch_bounds__(H * 4, 2) void fit_kernel(const FitArgs a, const fl
             return __uint_as_float(__float_as_uint(fmaxf(z, 0.0f)) & (unsigned)((int)(keep << (31 - bit)) >> 31));
         };
         const floatx16 zero = {0};
-        for (int k = 0; k < 4; ++k) meet();                 // the first samples are there
+        meet();                                             // the first samples are there
         for (int it = 0; it < mine; ++it) {
             const int now = it & 1;
             floatx16 z;
@@ -518,58 +589,7 @@ __global__ __launch_bounds__(H * 4, 2) void fit_kernel(const FitArgs a, const fl
         return;
     }
 
-    // ---- sums, and what is to come.  UB neighbouring lanes take the features of one side of a sample, EACH of them each; the first of these
-    // wavefronts ("scout") looks up what the samples name and what was measured of them, a side to either half of it.
-    constexpr int EACH = HALF / UB;
-    const int place = tid - 64 * UB, row = place / UB, sub = place % UB, own = row >> 1, side = row & 1;
-    const bool scout = ub == 0;
-    const float *const features = side ? a.X[1] : a.X[0];
-    const int all_features = (side ? a.rows[1] : a.rows[0]) > 0 ? (side ? a.rows[1] : a.rows[0]) * a.F : a.F;       // (at most 2^20 x 48)
-    float4v x[EACH / 4];
-    bool next_real = false;
-    // (the scout's: loads without a condition, from a place that is there anyway, so that nothing waits for them before they are needed)
-    const int32_t *const index = hh ? a.index[1] : a.index[0];
-    const float *const targets = hh ? a.target[1] : a.target[0], *const shares = hh ? a.X[1] : a.X[0];
-    const int share_feature = hh ? a.sm_feature[1] : a.sm_feature[0];
-    int looked = 0, named = -1;
-    float next_target = __builtin_nanf(""), next_share = 0.0f;
-    const auto sample_of = [&](const int it) { const long long s = tile_of(it) * T + nn; return s < a.count ? s : a.count - 1; };
-    const auto look = [&](const int it) { looked = index[sample_of(it)]; };
-    const auto name = [&](const int it) {                   // what has been looked up: a sample that names no pair has no part in anything
-        const bool mine_real = tile_of(it) * T + nn < a.count && (unsigned)looked < (unsigned)(hh ? a.rows[1] : a.rows[0]);
-        const auto both = __builtin_amdgcn_permlane32_swap((unsigned)mine_real, (unsigned)mine_real, false, false);
-        named = (both[0] & both[1]) ? looked : -1;
-        sh.pair[hh][nn] = named;
-    };
-    const auto ask = [&](const int it) {                    // what was measured, and the SM share, of the samples named last
-        if (targets) next_target = targets[sample_of(it)];
-        if (with_share) next_share = shares[(named < 0 ? 0 : named) * a.F + share_feature];
-    };
-    const auto answer = [&](const int it) {
-        const int to = it & 1;
-        sh.target[to][hh][nn] = named < 0 ? __builtin_nanf("") : next_target;
-        if (with_share) {
-            const auto both = __builtin_amdgcn_permlane32_swap(__float_as_uint(next_share), __float_as_uint(next_share), false, false);
-            const float share = fminf(1.0f - __uint_as_float(both[0]), __uint_as_float(both[1]));
-            if (hh == 0) sh.share[it & 3][nn] = named < 0 ? 0.0f : share;
-        }
-        if (hh == 0) sh.real[to][nn] = named >= 0;
-    };
-    const auto fetch = [&](const int part) {                // features of the samples named last, in two parts
-        const int at = sh.pair[side][own];
-        if (part == 0) next_real = at >= 0;
-        // (what a lane reads beyond its row is the next row's, and is left out when it is put to use; beyond the last row it reads nothing)
-        const int at_feature = (at < 0 ? 0 : at) * a.F + sub * EACH;
-#pragma unroll
-        for (int e = 0; e < EACH / 4; ++e) {
-            if (e % 2 != part) continue;
-            const int first = at_feature + 4 * e;
-            if (first + 4 <= all_features) x[e] = *(const float4v *)(features + first);
-            else
-#pragma unroll
-                for (int k = 0; k < 4; ++k) x[e][k] = features[first + k < all_features ? first + k : all_features - 1];
-        }
-    };
+    // ---- sums, and what is to come
     const auto stage = [&](const int it) {                  // what has been fetched, normalised, as pieces
         const int to = it & 1;
         float sum = 0.0f, mean = 0.0f, by = s_x;
@@ -617,27 +637,16 @@ __global__ __launch_bounds__(H * 4, 2) void fit_kernel(const FitArgs a, const fl
         sh.keep[it & 1][layer][s][k] = (unsigned char)(keep | keep >> 12);
     };
     static_assert(T * (H / 8) == 2 * 64 * UB, "groups");
-    if (scout) {
-        look(0);
-        const int first = looked;
-        look(1);
-        const int second = looked;
-        looked = first;
-        name(0);
-        ask(0);
-        looked = second;
-    }
-    meet();
-    fetch(0);
-    fetch(1);
     stage(0);
-    if (scout) answer(0);
-    meet();
-    if (scout) name(1);
-    meet();
-    fetch(0);
-    fetch(1);
-    if (scout) look(2);
+    if (scout) {
+        const int later = named;
+        named = named_first;
+        answer(0);
+        named = later;
+    }
+    fetch(1, 0);
+    fetch(1, 1);
+    if (scout) look(2, looked);
     if (a.drop) for (int q = 0; q < 4; ++q) draw(0, q);
     floatx16 gw2[GRAD ? UB : 1], gw1[GRAD ? CT : 1];
     float gb1 = 0.0f, gb2 = 0.0f, gsm = 0.0f, one = 1.0f;
@@ -719,22 +728,22 @@ __global__ __launch_bounds__(H * 4, 2) void fit_kernel(const FitArgs a, const fl
         draw_next(0)();
         meet();
         if (scout && more) answer(it + 1);
-        if (scout && it + 2 < mine) name(it + 2);
+        if (scout && it + 2 < mine) name(it + 2, looked);
         if (GRAD && it > 0) add_w1(it - 1, [] {});
         draw_next(1)();
         meet();
         draw_next(2)();
         if (more) stage(it + 1);
-        if (it + 2 < mine) fetch(0);
+        if (it + 2 < mine) fetch(it + 2, 0);
         if (!GRAD) {
             draw_next(3)();
-            if (it + 2 < mine) fetch(1);
-            if (scout) look(it + 3);
+            if (it + 2 < mine) fetch(it + 2, 1);
+            if (scout) look(it + 3, looked);
             continue;
         }
         meet();
-        if (it + 2 < mine) fetch(1);
-        if (scout) look(it + 3);
+        if (it + 2 < mine) fetch(it + 2, 1);
+        if (scout) look(it + 3, looked);
         add_w2(now, 0, draw_next(3));
         if (L::D1 == 1) add_w2(now, 1, [] {});
         meet();
@@ -776,6 +785,7 @@ __global__ __launch_bounds__(FIT_SUM_VALUES * FIT_SUM_SLICES) void fit_sum_kerne
     const int v = first + blockIdx.x * FIT_SUM_VALUES + place;
     float s = 0.0f;
     if (v < values)
+#pragma unroll 4
         for (int p = slice; p < o.parts; p += FIT_SUM_SLICES) s += partial[p * step + v];
     sums[slice][place] = s;
     __syncthreads();
@@ -814,6 +824,7 @@ __global__ __launch_bounds__(64 * UNFOLD_SLICES) void unfold_kernel(const float 
     const int lane = threadIdx.x % 64, slice = threadIdx.x / 64, c = blockIdx.x * 64 + lane, columns = 2 * F, from = c < F ? c : half + c - F;
     float weight = 0.0f, bias = 0.0f;
     if (c < columns)
+#pragma unroll 4
         for (int k = slice; k < H; k += UNFOLD_SLICES) {
             const float G1 = G[(size_t)k * padded + from], W = W1[(size_t)k * columns + c];
             dW1[(size_t)k * columns + c] = fmaf(G1, g[c], h[k] * beta[c]);
@@ -856,9 +867,9 @@ FitPlan fit_plan(const mf_ctx *ctx, const mf_predictor *p, long long count)
     return f;
 }
 
-// Where the folded layer 1 and what goes with it lie in the context's scratch (floats).
-constexpr int FOLD_BIAS = 128 * 512, FOLD_NORM1 = FOLD_BIAS + 128, FOLD_NORM2 = FOLD_NORM1 + 128, FOLD_RANGES = FOLD_NORM2 + 128, FOLD_SCALE = FOLD_RANGES + 2 * FIT_RANGE_PARTS;
-static_assert(FOLD_SCALE < MF_FIT_SCRATCH, "scratch");
+// Where what fold_kernel makes lies in the context's scratch (floats).
+constexpr int FOLD_BIAS = 128 * 512, FOLD_RANGES = FOLD_BIAS + 128;
+static_assert(FOLD_RANGES + FIT_RANGE_PARTS <= MF_FIT_SCRATCH, "scratch");
 
 template <int H, int CT, bool GRAD, bool EXTRA>
 int launch_fit(mf_ctx *ctx, const FitArgs &a, const FitPlan &f)
@@ -870,8 +881,7 @@ int launch_fit(mf_ctx *ctx, const FitArgs &a, const FitPlan &f)
         MF_HIP(hipFuncSetAttribute((const void *)fit_kernel<H, CT, GRAD, EXTRA>, hipFuncAttributeMaxDynamicSharedMemorySize, bytes));
         ctx->fit_configured |= flag;
     }
-    hipLaunchKernelGGL((fit_kernel<H, CT, GRAD, EXTRA>), dim3(f.grid), dim3(H * 4), bytes, ctx->stream, a, ctx->fit_W1 + FOLD_SCALE, ctx->fit_W1 + FOLD_NORM1,
-                       ctx->fit_W1 + FOLD_NORM2, ctx->fit_W1 + FOLD_RANGES, f.parts);
+    hipLaunchKernelGGL((fit_kernel<H, CT, GRAD, EXTRA>), dim3(f.grid), dim3(H * 4), bytes, ctx->stream, a, ctx->fit_W1 + FOLD_RANGES, f.parts);
     MF_HIP(hipGetLastError());
     return MF_OK;
 }
@@ -905,7 +915,8 @@ int run_fit(mf_ctx *ctx, const mf_predictor *p, const float *d_on, int n, const 
     a.target[0] = s->d_target; a.target[1] = s->d_target_slow;
     a.sigma[0] = d_sigma; a.sigma[1] = d_sigma_slow;
     a.count = s->count;
-    a.W1 = ctx->fit_W1; a.b1 = ctx->fit_W1 + FOLD_BIAS;
+    a.W1 = f.wide ? ctx->fit_W1 : p->d_W1; a.b1 = f.wide ? ctx->fit_W1 + FOLD_BIAS : p->d_b1;
+    a.g = p->d_ln_w; a.beta = p->d_ln_b;
     a.W2 = p->d_W2; a.b2 = p->d_b2;
     a.W3[0] = p->d_W3; a.W3[1] = p->d_W3_slow;
     a.b3[0] = p->d_b3; a.b3[1] = p->d_b3_slow;
@@ -916,24 +927,21 @@ int run_fit(mf_ctx *ctx, const mf_predictor *p, const float *d_on, int n, const 
     if (a.drop) { a.rule = *rule; a.step = (const unsigned long long *)d_step; }
     a.partial = (float *)d_work;
     a.partial_step = f.step(g != nullptr);
-    FoldArgs w{};
-    w.W1 = p->d_W1; w.b1 = p->d_b1; w.g = p->d_ln_w; w.beta = p->d_ln_b;
-    w.H = f.H; w.F = p->F; w.padded = f.padded; w.half = f.half; w.wide = f.wide;
-    w.image = ctx->fit_W1; w.bias = ctx->fit_W1 + FOLD_BIAS; w.scale = ctx->fit_W1 + FOLD_SCALE;
-    w.norm1 = ctx->fit_W1 + FOLD_NORM1; w.norm2 = ctx->fit_W1 + FOLD_NORM2; w.ranges = ctx->fit_W1 + FOLD_RANGES;
-    for (int k = 0; k < 2; ++k) { w.target[k] = a.target[k]; w.X[k] = a.X[k]; w.index[k] = a.index[k]; w.rows[k] = a.rows[k]; }
-    w.count = a.count;
-    // (as many features are looked at as there are, or as the samples name, whichever is fewer)
-    w.features = f.wide || (a.norm && !a.W1sm) ? 0 : 2 * s->count < (long long)n + m ? 2 : 1;
-    if (!f.wide) {                                          // eight values a thread
-        long long values = (a.target[0] ? a.count : 0) + (a.target[1] ? a.count : 0);
-        if (w.features) values += p->F * (w.features == 2 ? 2 * a.count : (long long)n + m);
-        const long long parts = (values + 2047) / 2048;
-        f.parts = (int)(parts < 1 ? 1 : parts < FIT_RANGE_PARTS ? parts : FIT_RANGE_PARTS);
+    const bool bounded = a.norm && !a.W1sm;                 // (a norm bounds what it gives)
+    if (f.wide || !bounded) {
+        FoldArgs w{};
+        w.W1 = p->d_W1; w.b1 = p->d_b1; w.g = p->d_ln_w; w.beta = p->d_ln_b;
+        w.F = p->F; w.padded = f.padded; w.wide = f.wide;
+        w.W = ctx->fit_W1; w.bias = ctx->fit_W1 + FOLD_BIAS; w.ranges = ctx->fit_W1 + FOLD_RANGES;
+        w.width = a.norm ? 1 : p->F;
+        for (int k = 0; k < 2; ++k) { w.X[k] = a.X[k]; w.index[k] = a.index[k]; w.rows[k] = a.rows[k]; w.first[k] = a.norm ? a.sm_feature[k] : 0; }
+        w.count = a.count;
+        w.listed = 2 * s->count < (long long)n + m;
+        const long long values = w.width * (w.listed ? 2 * a.count : (long long)n + m), parts = (values + 2047) / 2048;      // eight values a thread
+        f.parts = w.parts = f.wide ? 0 : (int)(parts < 1 ? 1 : parts < FIT_RANGE_PARTS ? parts : FIT_RANGE_PARTS);
+        hipLaunchKernelGGL(fold_kernel, dim3(f.wide ? f.H / 4 : w.parts), dim3(256), 0, ctx->stream, w);
+        MF_HIP(hipGetLastError());
     }
-    w.parts = f.parts;
-    hipLaunchKernelGGL(fold_kernel, dim3(f.H / 4 + f.parts), dim3(256), 0, ctx->stream, w);
-    MF_HIP(hipGetLastError());
     const int rc = f.wide ? mf_launch_wide(ctx, a, f, g != nullptr) : f.H == 64 ? launch_fit_for<64>(ctx, a, f, g != nullptr) : launch_fit_for<128>(ctx, a, f, g != nullptr);
     if (rc != MF_OK || !a.partial) return rc;
     FitOut o{};

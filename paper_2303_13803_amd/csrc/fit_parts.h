@@ -8,7 +8,7 @@
 typedef float floatx16 __attribute__((ext_vector_type(16)));
 
 constexpr int FIT_WIDE_FROM = 49;                           // features a workload from which on fit_wide.hip takes over
-constexpr int FIT_RANGE_PARTS = 256;                        // workgroups that look at most for the largest target and feature
+constexpr int FIT_RANGE_PARTS = 256;                        // workgroups that look for the largest feature, at most
 
 struct FitArgs {
     const float *X[2];
@@ -17,7 +17,7 @@ struct FitArgs {
     const float *target[2];                                 // throughput, slowdown (null: not trained)
     float *sigma[2];                                        // (null: not wanted)
     long long count;
-    const float *W1, *b1;                                   // layer 1 with the norm folded in (see fold_kernel)
+    const float *W1, *b1, *g, *beta;                        // wide: layer 1 with the norm folded in (see fold_kernel)
     const float *W2, *b2, *W3[2], *b3[2], *W1sm;            // ([1] and W1sm may be null)
     int norm, sm_feature[2];
     float eps;
