@@ -47,13 +47,15 @@ class Samples(C.Structure):
                 ("count", C.c_int64)]
 
 
-# members of mf_gradients and the names their parameters have in a predictor's dictionary
-PARAMETERS = (("d_W1", "W1"), ("d_b1", "b1"), ("d_W2", "W2"), ("d_b2", "b2"), ("d_W3", "W3"), ("d_b3", "b3"),
-              ("d_W1sm", "W1sm"), ("d_W3_slow", "W3slow"), ("d_b3_slow", "b3slow"), ("d_ln_w", "ln_w"), ("d_ln_b", "ln_b"))
+# members of mf_gradients, the names their parameters have in a predictor's dictionary, and their sizes for F features and H hidden units
+PARAMETERS = (("d_W1", "W1", lambda F, H: 2 * F * H), ("d_b1", "b1", lambda F, H: H), ("d_W2", "W2", lambda F, H: H * H),
+              ("d_b2", "b2", lambda F, H: H), ("d_W3", "W3", lambda F, H: H), ("d_b3", "b3", lambda F, H: 1),
+              ("d_W1sm", "W1sm", lambda F, H: H), ("d_W3_slow", "W3slow", lambda F, H: H), ("d_b3_slow", "b3slow", lambda F, H: 1),
+              ("d_ln_w", "ln_w", lambda F, H: 2 * F), ("d_ln_b", "ln_b", lambda F, H: 2 * F))
 
 
 class Gradients(C.Structure):
-    _fields_ = [(member, C.c_void_p) for member, _ in PARAMETERS]
+    _fields_ = [(member, C.c_void_p) for member, _, _ in PARAMETERS]
 
 
 LAYER_TYPES = {torch.float32: 0, torch.float16: 1, torch.bfloat16: 2}
@@ -171,7 +173,11 @@ class Context:
         """Pointer of a contiguous tensor of `count` values on this context's device."""
         if t is None and optional:
             return None
-        if not isinstance(t, torch.Tensor) or t.get_device() != self.device or t.dtype != dtype or not t.is_contiguous():
+        try:
+            fits = t.dtype == dtype and t.get_device() == self.device and t.is_contiguous()
+        except AttributeError:
+            fits = False
+        if not fits:
             raise TypeError(f"{what}: expected a contiguous tensor of {dtype} on device {self.device}")
         if t.numel() != count:
             raise ValueError(f"{what}: expected {count} values, got {t.numel()}")
@@ -179,10 +185,13 @@ class Context:
 
     def _rows(self, t, kind, shape, what):
         """(pointer, pitch) of a matrix of this type and shape whose rows may lie apart but whose values lie side by side."""
-        if not isinstance(t, torch.Tensor) or t.get_device() != self.device:
-            raise TypeError(f"{what}: expected a tensor on device {self.device}")
-        if t.dtype != kind or t.shape != shape:
-            raise ValueError(f"{what}: expected a matrix of the input's shape and type")
+        try:
+            if t.get_device() != self.device:
+                raise TypeError(f"{what}: expected a tensor on device {self.device}")
+            if t.dtype != kind or t.shape != shape:
+                raise ValueError(f"{what}: expected a matrix of the input's shape and type")
+        except AttributeError:
+            raise TypeError(f"{what}: expected a tensor on device {self.device}") from None
         pitch, step = t.stride()
         rows, width = shape
         if rows < 2:
@@ -198,14 +207,14 @@ class Context:
             raise TypeError(f"{what}: expected a float32, float16 or bfloat16 matrix")
         return kind, LAYER_TYPES[kind], t.shape
 
-    def _work(self, work, needed):
-        """The caller's scratch, or as much from torch's allocator, in the order of this context's stream."""
-        if needed < 0:
-            raise MuxmatchError(int(needed))
+    def _work(self, work, needed, *args):
+        """The caller's scratch (the call itself looks at its size), or needed(*args) bytes from torch's allocator, in the order of this
+        context's stream."""
         if work is None:
+            size = needed(*args)
             with torch.cuda.stream(self.stream):
-                work = torch.empty(max(int(needed), 16), dtype=torch.uint8, device=f"cuda:{self.device}")
-        elif not isinstance(work, torch.Tensor) or not work.is_cuda or work.device.index != self.device or work.dtype != torch.uint8 or not work.is_contiguous():
+                return torch.empty(max(size, 16), dtype=torch.uint8, device=f"cuda:{self.device}")
+        if not isinstance(work, torch.Tensor) or work.dtype != torch.uint8 or work.get_device() != self.device or not work.is_contiguous():
             raise TypeError(f"work: expected a contiguous tensor of torch.uint8 on device {self.device}")
         return work
 
@@ -241,7 +250,7 @@ class Context:
         pdy, lddy = self._rows(dy, kind, shape, "dy")
         pdx, lddx = self._rows(dx, kind, shape, "dx")
         rows, width = shape
-        work = self._work(work, _lib.mf_layer_norm_grad_work(self._h, rows, width))
+        work = self._work(work, self.layer_norm_grad_work, rows, width)
         flat = lambda t, what: self._flat(t, torch.float32, width, what)
         self._check(_lib.mf_layer_norm_grad(self._h, number, px, rows, width, ldx, pdy, lddy,
                                             flat(weight, "weight"), float(eps), pdx, lddx, flat(dweight, "dweight"),
@@ -286,12 +295,10 @@ class Context:
                           self._flat(target, torch.float32, count, "target"), flat(target_slow, "target_slow"), count)
         rule = self._dropout(*dropout, *((0,) if len(dropout) == 2 else ())) if dropout is not None else None
         if grads is not None:
-            pointers = []
-            for member, name in PARAMETERS:
-                has = getattr(pred, member) is not None
-                pointers.append(self._flat(grads[name], torch.float32, pred._keep[name].numel(), f"grads[{name!r}]") if has else None)
-            grads = Gradients(*pointers)
-        work = self._work(work, _lib.mf_predictor_loss_work(self._h, C.byref(pred), count))
+            F, H = pred.F, pred.H
+            grads = Gradients(*[self._flat(grads[name], torch.float32, size(F, H), name) if getattr(pred, member) is not None else None
+                                for member, name, size in PARAMETERS])
+        work = self._work(work, self.predictor_loss_work, pred, count)
         self._check(_lib.mf_predictor_loss(
             self._h, C.byref(pred), *sides, C.byref(samples), C.byref(rule) if rule is not None else None,
             1.0 / max(count, 1) if scale is None else float(scale), C.byref(grads) if grads is not None else None,

@@ -141,7 +141,7 @@ __device__ __forceinline__ void meet()
 // Everything of a workgroup's that wavefronts share.
 template <int H, int CT, bool GRAD>
 struct FitShared {
-    static constexpr int T = FIT_ROWS, UB = H / 32, KB = H / 16, XN = CT == 3 ? 16 : 4 * CT;
+    static constexpr int T = FIT_ROWS, UB = H / 32, KB = H / 16, XN = CT >= 3 ? 16 : 4 * CT;
     // d1 of the samples before is kept for a stage longer where there is room for it
     static constexpr int D1 = GRAD && (H == 64 || CT < 3) ? 2 : 1;
     Rows<H / 8> d1[D1][2], dz2[GRAD ? 2 : 1], dz1[GRAD ? 2 : 1];    // [of which samples][piece]
@@ -237,7 +237,7 @@ __global__ __launch_bounds__(H * 4, 2) void fit_kernel(const FitArgs a, const fl
     const int place = tid - 64 * UB, row = place / UB, sub = place % UB, own = row >> 1, side = row & 1;
     const bool scout = ub == 0;
     const float *const features = side ? a.X[1] : a.X[0];
-    const int all_features = (side ? a.rows[1] : a.rows[0]) > 0 ? (side ? a.rows[1] : a.rows[0]) * a.F : a.F;       // (at most 2^20 x 48)
+    const int all_features = (side ? a.rows[1] : a.rows[0]) > 0 ? (side ? a.rows[1] : a.rows[0]) * a.F : a.F;       // (at most 2^20 x 64)
     float4v x[EACH / 4];
     bool next_real = false;
     // (the scout's: loads without a condition, from a place that is there anyway, so that nothing waits for them before they are needed)
@@ -890,7 +890,8 @@ template <int H, bool GRAD, bool EXTRA>
 int launch_fit_tiles(mf_ctx *ctx, const FitArgs &a, const FitPlan &f)
 {
     if (f.tiles == 1) return launch_fit<H, 1, GRAD, EXTRA>(ctx, a, f);
-    return f.tiles == 2 ? launch_fit<H, 2, GRAD, EXTRA>(ctx, a, f) : launch_fit<H, 3, GRAD, EXTRA>(ctx, a, f);
+    if (f.tiles == 2) return launch_fit<H, 2, GRAD, EXTRA>(ctx, a, f);
+    return f.tiles == 3 ? launch_fit<H, 3, GRAD, EXTRA>(ctx, a, f) : launch_fit<H, 4, GRAD, EXTRA>(ctx, a, f);
 }
 
 template <int H>

@@ -7,7 +7,7 @@
 
 typedef float floatx16 __attribute__((ext_vector_type(16)));
 
-constexpr int FIT_WIDE_FROM = 49;                           // features a workload from which on fit_wide.hip takes over
+constexpr int FIT_WIDE_FROM = 65;                           // features a workload from which on fit_wide.hip takes over
 constexpr int FIT_RANGE_PARTS = 256;                        // workgroups that look for the largest feature, at most
 
 struct FitArgs {

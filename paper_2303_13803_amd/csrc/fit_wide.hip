@@ -1,4 +1,4 @@
-// The pass over the samples of a predictor of many features (49 to 256 a workload), in float32 products: features are staged 64 columns at a time, twice a
+// The pass over the samples of a predictor of many features (65 to 256 a workload), in float32 products: features are staged 64 columns at a time, twice a
 // sample, and gradients of layer 1 are kept for 256 columns at a time, which is as many as there are accumulators for: more take another pass over
 // the samples each.  See fit.hip for what is computed.
 #include "fit_parts.h"

@@ -214,7 +214,7 @@ __global__ __launch_bounds__(LAYER_THREADS) void norm_grad_kernel(NormArgs a)
 }
 
 // out[0][c] and out[1][c] = the sums of partial[.][0][c] and partial[.][1][c].
-constexpr int SUM_COLUMNS = 64, SUM_SLICES = 16;
+constexpr int SUM_COLUMNS = 32, SUM_SLICES = 32;
 
 __global__ __launch_bounds__(SUM_COLUMNS * SUM_SLICES) void column_sum_kernel(const float *__restrict__ partial, int parts, int width, float *dw, float *db)
 {
@@ -222,6 +222,7 @@ __global__ __launch_bounds__(SUM_COLUMNS * SUM_SLICES) void column_sum_kernel(co
     const int c = blockIdx.x * SUM_COLUMNS + threadIdx.x % SUM_COLUMNS, slice = threadIdx.x / SUM_COLUMNS;
     float s = 0.0f;
     if (c < 2 * width)
+#pragma unroll 8
         for (int p = slice; p < parts; p += SUM_SLICES) s += partial[(int64_t)p * 2 * width + c];
     sums[slice][threadIdx.x % SUM_COLUMNS] = s;
     __syncthreads();
@@ -240,8 +241,13 @@ void launch_norm(const mf_ctx *ctx, const NormArgs &a, int grid)
 
 int least(int64_t a, int64_t b) { return (int)(a < b ? a : b); }
 
-// Workgroups of the gradient: eight rows at least for each, so that the sums they leave are a small part of what they read.
-int norm_grad_parts(const mf_ctx *ctx, int64_t rows) { return least((rows + 7) / 8, 2ll * (ctx->n_cus > 0 ? ctx->n_cus : 256)); }
+// Workgroups of the gradient: rows enough for each that the sums they leave are a small part of what they read, and four to a compute
+// unit, as many as registers let in.
+int norm_grad_parts(const mf_ctx *ctx, int64_t rows, int64_t width)
+{
+    const int64_t each = width >= 256 ? 8 : width <= 8 ? 256 : 2048 / width;
+    return least((rows + each - 1) / each, 4ll * (ctx->n_cus > 0 ? ctx->n_cus : 256));
+}
 
 // As few lanes a row as hold it in one vector each, so that narrow rows share a wavefront; then more vectors a lane, and beyond
 // 64 lanes x 4 vectors (2 of a 16-bit type) a whole workgroup.  Rows narrower than one vector go value by value.
@@ -250,7 +256,7 @@ void launch_norm_for(const mf_ctx *ctx, const NormArgs &a)
 {
     constexpr int V = 16 / sizeof(T), WIDE = sizeof(T) == 4 ? 4 : 2;
     const int vectors = (a.width + V - 1) / V, units = ctx->n_cus > 0 ? ctx->n_cus : 256;
-    const int parts = GRAD ? norm_grad_parts(ctx, a.rows) : 0;
+    const int parts = GRAD ? norm_grad_parts(ctx, a.rows, a.width) : 0;
     const auto grid = [&](int lanes) {
         const int64_t needed = (a.rows + LAYER_THREADS / lanes - 1) / (LAYER_THREADS / lanes);
         return GRAD ? parts : least(needed, (int64_t)units * 8);
@@ -384,7 +390,7 @@ int mf_layer_norm(mf_ctx *ctx, int type, const void *d_x, int64_t rows, int64_t 
 int64_t mf_layer_norm_grad_work(mf_ctx *ctx, int64_t rows, int64_t width)
 {
     const int rc = check_rows(ctx, MF_F32, rows, width);
-    return rc != MF_OK ? rc : (int64_t)norm_grad_parts(ctx, rows) * 2 * width * (int64_t)sizeof(float);
+    return rc != MF_OK ? rc : (int64_t)norm_grad_parts(ctx, rows, width) * 2 * width * (int64_t)sizeof(float);
 }
 
 int mf_layer_norm_grad(mf_ctx *ctx, int type, const void *d_x, int64_t rows, int64_t width, int64_t ldx,
@@ -407,7 +413,7 @@ int mf_layer_norm_grad(mf_ctx *ctx, int type, const void *d_x, int64_t rows, int
     a.partial = (float *)d_work;
     if (rows > 0) launch_norm_type<true>(ctx, type, a);
     hipLaunchKernelGGL(column_sum_kernel, dim3((unsigned)((2 * width + SUM_COLUMNS - 1) / SUM_COLUMNS)), dim3(SUM_COLUMNS * SUM_SLICES), 0, ctx->stream,
-                       a.partial, rows > 0 ? norm_grad_parts(ctx, rows) : 0, (int)width, d_dw, d_db);
+                       a.partial, rows > 0 ? norm_grad_parts(ctx, rows, width) : 0, (int)width, d_dw, d_db);
     MF_HIP(hipGetLastError());
     return MF_OK;
 }

@@ -154,7 +154,7 @@ def _predictor(lib, **change):
 def _loss(lib, ctx, pred=(), samples=(), grads=(), **change):
     p = _predictor(lib, **dict(pred))
     s = lib.Samples(*{**dict(d_on=A, d_off=A, d_target=A, d_target_slow=None, count=100), **dict(samples)}.values())
-    g = lib.Gradients(*{**{m: A for m, _ in lib.PARAMETERS}, **dict(grads)}.values())
+    g = lib.Gradients(*{**{m: A for m, *_ in lib.PARAMETERS}, **dict(grads)}.values())
     a = dict(predictor=C.byref(p), x_on=A, n=5, x_off=A, m=5, listed=C.byref(s), dropout=None, scale=0.01, grads=C.byref(g), loss=A, sigma=A, sigma_slow=None,
              work=A, bytes=1 << 30)
     return lib.raw_library().mf_predictor_loss(ctx, *{**a, **change}.values())
