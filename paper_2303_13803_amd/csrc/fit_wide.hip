@@ -48,7 +48,8 @@ __global__ __launch_bounds__(H * 4) void wide_kernel(const FitArgs a)
     const int pass_chunk = blockIdx.y * GT;                 // this pass keeps gradients of layer 1 from this chunk on
 
     floatx16 gw2[UB / 2], gw1[GT];
-    // sums of the 16 units of a half over the wavefront's samples: lane nn of a half keeps that of unit nn
+    // gw3, gw3s: sums of the 16 units of a half over the wavefront's samples, lane nn of a half keeps that of unit nn; gb1, gb2, gsm: of unit
+    // 32 ub + nn over all of the workgroup's that this half reads
     float gb1 = 0.0f, gb2 = 0.0f, gw3 = 0.0f, gw3s = 0.0f, gsm = 0.0f, gb3 = 0.0f, gb3s = 0.0f, loss = 0.0f;
     if (GRAD) {
 #pragma unroll
@@ -59,33 +60,44 @@ __global__ __launch_bounds__(H * 4) void wide_kernel(const FitArgs a)
             for (int t = 0; t < GT; ++t) gw1[t][e] = 0.0f;
         }
     }
-    // features of columns 64 chunk .. 64 chunk + 63
-    auto stage = [&](const int chunk) {
-        for (int e = tid; e < T * FIT_CHUNK; e += THREADS) {
-            const int s = e / FIT_CHUNK, c = chunk * FIT_CHUNK + e % FIT_CHUNK, side = c >= a.F;
-            float v = 0.0f;
-            if (c < a.columns && at_on[s] >= 0) {
-                const float2 m = moments[2 * s + side];
-                v = ((side ? a.X[1] : a.X[0])[(size_t)(side ? at_off[s] : at_on[s]) * a.F + c - (side ? a.F : 0)] - m.x) * m.y;
-            }
-            xs[s * XP + e % FIT_CHUNK] = v;
+    // Features of columns 64 chunk .. 64 chunk + 63 are fetched a stage before they are laid into LDS (waited for one by one they took 12 us a
+    // chunk, together 3).
+    constexpr int EACH_FEATURE = T * FIT_CHUNK / THREADS;
+    float feature[EACH_FEATURE];
+    auto fetch = [&](const int chunk) {
+        const int c = chunk * FIT_CHUNK + tid % FIT_CHUNK, side = c >= a.F;
+        const float *X = side ? a.X[1] + (c - a.F) : a.X[0] + c;
+#pragma unroll
+        for (int k = 0; k < EACH_FEATURE; ++k) {
+            const int s = tid / FIT_CHUNK + k * (THREADS / FIT_CHUNK), at = side ? at_off[s] : at_on[s];
+            feature[k] = c < a.columns && at >= 0 ? X[(size_t)at * a.F] : 0.0f;
+        }
+    };
+    auto lay = [&](const int chunk) {
+        const int c = chunk * FIT_CHUNK + tid % FIT_CHUNK, side = c >= a.F;
+#pragma unroll
+        for (int k = 0; k < EACH_FEATURE; ++k) {
+            const int s = tid / FIT_CHUNK + k * (THREADS / FIT_CHUNK);
+            const float2 m = moments[2 * s + side];
+            xs[s * XP + tid % FIT_CHUNK] = c < a.columns && at_on[s] >= 0 ? (feature[k] - m.x) * m.y : 0.0f;
         }
     };
     // bias, ReLU and dropout of this lane's 16 units of one layer
     auto activate = [&](const floatx16 &z, float (&h)[16], const float *bias, const float share_here, long long sample, unsigned layer) {
 #pragma unroll
-        for (int g = 0; g < 2; ++g) {
-            Words4 bits;
-            if (a.drop) bits = drop_bits(rule, (unsigned long long)sample * (H / 8) + (u0 + 16 * g) / 8, layer);
+        for (int k = 0; k < 16; ++k) h[k] = z[k] + bias[u0 + 16 * (k >> 3) + (k & 7)];
+        if (layer == 0 && a.W1sm)
 #pragma unroll
-            for (int e = 0; e < 8; ++e) {
-                float v = z[8 * g + e] + bias[u0 + 16 * g + e];
-                if (layer == 0 && a.W1sm) v = fmaf(share_here, vec[4 * H + u0 + 16 * g + e], v);
-                v = relu(v);
-                if (a.drop) v = drop_keeps(rule, bits, e) ? v * factor : 0.0f;
-                h[8 * g + e] = v;
+            for (int k = 0; k < 16; ++k) h[k] = fmaf(share_here, vec[4 * H + u0 + 16 * (k >> 3) + (k & 7)], h[k]);
+#pragma unroll
+        for (int k = 0; k < 16; ++k) h[k] = relu(h[k]);
+        if (a.drop)
+#pragma unroll
+            for (int g = 0; g < 2; ++g) {
+                const Words4 bits = drop_bits(rule, (unsigned long long)sample * (H / 8) + (u0 + 16 * g) / 8, layer);
+#pragma unroll
+                for (int e = 0; e < 8; ++e) h[8 * g + e] = drop_keeps(rule, bits, e) ? h[8 * g + e] * factor : 0.0f;
             }
-        }
     };
     auto add_lane = [&](float &sum, const int k, const float v) {
         const float all = group_sum<32>(v);
@@ -116,6 +128,7 @@ __global__ __launch_bounds__(H * 4) void wide_kernel(const FitArgs a)
             share[tid] = i >= 0 && a.W1sm ? fminf(1.0f - a.X[0][(size_t)i * a.F + a.sm_feature[0]], a.X[1][(size_t)j * a.F + a.sm_feature[1]]) : 0.0f;
         }
         __syncthreads();
+        fetch(0);
         {   // moments of the samples' feature rows, 2 T of them, by THREADS / (2 T) neighbouring lanes each
             constexpr int EACH = THREADS / (2 * T);
             const int r = tid / EACH, sub = tid % EACH, side = r & 1;
@@ -124,8 +137,10 @@ __global__ __launch_bounds__(H * 4) void wide_kernel(const FitArgs a)
             if (a.norm && at >= 0) {                        // (the lanes of a row agree)
                 const float *x = (side ? a.X[1] : a.X[0]) + (size_t)at * a.F;
                 float sum = 0.0f, squares = 0.0f;
+#pragma unroll 8
                 for (int f = sub; f < a.F; f += EACH) sum += x[f];
                 m.x = group_sum<EACH>(sum) / (float)a.F;
+#pragma unroll 8
                 for (int f = sub; f < a.F; f += EACH) { const float d = x[f] - m.x; squares = fmaf(d, d, squares); }
                 m.y = 1.0f / sqrtf(group_sum<EACH>(squares) / (float)a.F + a.eps);
             }
@@ -137,11 +152,18 @@ __global__ __launch_bounds__(H * 4) void wide_kernel(const FitArgs a)
         for (int e = 0; e < 16; ++e) z[e] = 0.0f;
         for (int c = 0; c < chunks; ++c) {
             if (c > 0) __syncthreads();
-            stage(c);
-            __syncthreads();
             const int quads = (a.padded - c * FIT_CHUNK < FIT_CHUNK ? a.padded - c * FIT_CHUNK : FIT_CHUNK) / 8;
-            for (int q = 0; q < quads; ++q) {
-                const float4 w = *(const float4 *)(a.W1 + (size_t)unit * a.padded + c * FIT_CHUNK + 8 * q + 4 * hh);
+            float4 w1[FIT_CHUNK / 8];                       // (on their way while features are staged)
+#pragma unroll
+            for (int q = 0; q < FIT_CHUNK / 8; ++q)
+                w1[q] = *(const float4 *)(a.W1 + (size_t)unit * a.padded + c * FIT_CHUNK + (q < quads ? 8 * q : 0) + 4 * hh);
+            lay(c);
+            __syncthreads();
+            if (c + 1 < chunks) fetch(c + 1);
+#pragma unroll
+            for (int q = 0; q < FIT_CHUNK / 8; ++q) {
+                if (q >= quads) break;
+                const float4 w = w1[q];
                 const float4 x = *(const float4 *)(xs + mine * XP + 8 * q + 4 * hh);
                 z = __builtin_amdgcn_mfma_f32_32x32x2f32(w.x, x.x, z, 0, 0, 0);
                 z = __builtin_amdgcn_mfma_f32_32x32x2f32(w.y, x.y, z, 0, 0, 0);
@@ -157,6 +179,7 @@ __global__ __launch_bounds__(H * 4) void wide_kernel(const FitArgs a)
         __syncthreads();
 #pragma unroll
         for (int e = 0; e < 16; ++e) z[e] = 0.0f;
+#pragma unroll 2
         for (int q = 0; q < QUADS; ++q) {
             const float4 w = *(const float4 *)(w2 + unit * PITCH + 8 * q + 4 * hh);
             const float4 x = *(const float4 *)(act + mine * PITCH + 8 * q + 4 * hh);
@@ -197,23 +220,23 @@ __global__ __launch_bounds__(H * 4) void wide_kernel(const FitArgs a)
         if (speaks) { gb3 += dz; gb3s += dzs; }
         float d[16];
 #pragma unroll
-        for (int g = 0; g < 2; ++g)
+        for (int k = 0; k < 16; ++k) {
+            d[k] = dz * vec[2 * H + u0 + 16 * (k >> 3) + (k & 7)];
+            add_lane(gw3, k, dz * h2[k]);
+        }
+        if (a.W3[1])
 #pragma unroll
-            for (int e = 0; e < 8; ++e) {
-                const int k = 8 * g + e;
-                float v = dz * vec[2 * H + u0 + 16 * g + e];
-                add_lane(gw3, k, dz * h2[k]);
-                if (a.W3[1]) {
-                    v = fmaf(dzs, vec[3 * H + u0 + 16 * g + e], v);
-                    add_lane(gw3s, k, dzs * h2[k]);
-                }
-                d[k] = h2[k] > 0.0f ? v * factor : 0.0f;
-                add_lane(gb2, k, d[k]);
+            for (int k = 0; k < 16; ++k) {
+                d[k] = fmaf(dzs, vec[3 * H + u0 + 16 * (k >> 3) + (k & 7)], d[k]);
+                add_lane(gw3s, k, dzs * h2[k]);
             }
+#pragma unroll
+        for (int k = 0; k < 16; ++k) d[k] = h2[k] > 0.0f ? d[k] * factor : 0.0f;
         put(back, d);
         __syncthreads();
 #pragma unroll
         for (int e = 0; e < 16; ++e) z[e] = 0.0f;
+#pragma unroll 2
         for (int q = 0; q < QUADS; ++q) {                   // W2^T dz2
             const float *w = w2 + (8 * q + 4 * hh) * PITCH + unit;
             const float4 x = *(const float4 *)(back + mine * PITCH + 8 * q + 4 * hh);
@@ -223,17 +246,16 @@ __global__ __launch_bounds__(H * 4) void wide_kernel(const FitArgs a)
             z = __builtin_amdgcn_mfma_f32_32x32x2f32(w[3 * PITCH], x.w, z, 0, 0, 0);
         }
 #pragma unroll
-        for (int k = 0; k < 16; ++k) {
-            d[k] = h1[k] > 0.0f ? z[k] * factor : 0.0f;
-            add_lane(gb1, k, d[k]);
-            if (a.W1sm) add_lane(gsm, k, share[mine] * d[k]);
-        }
+        for (int k = 0; k < 16; ++k) d[k] = h1[k] > 0.0f ? z[k] * factor : 0.0f;
+        if (chunks > 1) fetch(pass_chunk);
         // sums over samples: the lower half of a wavefront takes sample 16 b + i, the upper one 16 b + 8 + i
+#pragma unroll 1
         for (int b = 0; b < T / 16; ++b)
 #pragma unroll
             for (int i = 0; i < 8; ++i) {
                 const int s = (16 * b + i + 8 * hh) * PITCH;
                 const float v = back[s + 32 * ub + nn];
+                gb2 += v;
 #pragma unroll
                 for (int t = 0; t < UB / 2; ++t)
                     gw2[t] = __builtin_amdgcn_mfma_f32_32x32x2f32(v, act[s + 32 * (sh + 2 * t) + nn], gw2[t], 0, 0, 0);
@@ -247,14 +269,21 @@ __global__ __launch_bounds__(H * 4) void wide_kernel(const FitArgs a)
             if (c >= chunks) break;
             if (chunks > 1) {
                 if (t > 0) __syncthreads();
-                stage(c);
+                lay(c);
                 __syncthreads();
+                if (t + 1 < GT && c + 1 < chunks) fetch(c + 1);
             }
             if (c * FIT_CHUNK + 32 * sh >= a.padded) continue;      // (the last chunk may be half as wide)
+#pragma unroll 1
             for (int b = 0; b < T / 16; ++b)
 #pragma unroll
                 for (int i = 0; i < 8; ++i) {
                     const int s = 16 * b + i + 8 * hh;
+                    if (t == 0) {
+                        const float v = act[s * PITCH + 32 * ub + nn];
+                        gb1 += v;
+                        gsm = fmaf(share[s], v, gsm);
+                    }
                     gw1[t] = __builtin_amdgcn_mfma_f32_32x32x2f32(act[s * PITCH + 32 * ub + nn], xs[s * XP + 32 * sh + nn], gw1[t], 0, 0, 0);
                 }
         }
@@ -277,16 +306,23 @@ __global__ __launch_bounds__(H * 4) void wide_kernel(const FitArgs a)
         for (int t = 0; t < UB / 2; ++t)
 #pragma unroll
             for (int e = 0; e < 16; ++e) out[S::W2 + (32 * ub + 8 * (e >> 2) + row + (e & 3)) * H + 32 * (sh + 2 * t) + nn] = gw2[t][e];
-        // sums of a unit over the lanes that hold it, then over the two wavefronts that do
-        float *sums = act;                                  // [5][2][H]
+        gb1 = both_halves(gb1);
+        gb2 = both_halves(gb2);
+        gsm = both_halves(gsm);
+        if (sh == 0 && hh == 0) {
+            out[S::B1 + 32 * ub + nn] = gb1;
+            out[S::B2 + 32 * ub + nn] = gb2;
+            out[S::SM + 32 * ub + nn] = gsm;
+        }
+        // the output weights': over the two wavefronts that hold a unit
+        float *sums = act;                                  // [2][2][H]
         __syncthreads();
-        const float v[5] = {gb1, gb2, gw3, gw3s, gsm};
-#pragma unroll
-        for (int q = 0; q < 5; ++q)
-            if (nn < 16) sums[(2 * q + sh) * H + u0 + (nn >> 3) * 16 + (nn & 7)] = v[q];
+        if (nn < 16) {
+            sums[sh * H + u0 + (nn >> 3) * 16 + (nn & 7)] = gw3;
+            sums[(2 + sh) * H + u0 + (nn >> 3) * 16 + (nn & 7)] = gw3s;
+        }
         __syncthreads();
-        for (int e = tid; e < 5 * H; e += THREADS) out[S::B1 + e] = sums[(2 * (e / H)) * H + e % H] + sums[(2 * (e / H) + 1) * H + e % H];
-        __syncthreads();
+        for (int e = tid; e < 2 * H; e += THREADS) out[S::W3 + e] = sums[2 * (e / H) * H + e % H] + sums[(2 * (e / H) + 1) * H + e % H];
     }
     const float v[3] = {group_sum<64>(gb3), group_sum<64>(gb3s), group_sum<64>(loss)};
     __syncthreads();
