@@ -485,7 +485,9 @@ typedef struct {
  * (the first) or 1.  grads may be NULL: the loss alone, as for validation.
  * d_sigma and d_sigma_slow ([count], either may be NULL) receive the predictions, with the same dropout; 0 for a
  * sample that names no pair.  Gradients are sums in a fixed order: the same call gives the same bits.
- * A ReLU passes no gradient at 0.  d_work as in mf_layer_norm_grad.
+ * A ReLU passes no gradient at 0.  d_work as in mf_layer_norm_grad.  What is written must not overlap what is read.
+ * Products take float32 operands to 22 bits or, of weights, features behind a norm and what is passed back, to 2^-39 of the largest of
+ * their kind in the call where that is more, and are added up in float32.
  * scale, mem_feature, mem_limit and slow_limit of the predictor play no part but have to be valid.
  */
 int64_t mf_predictor_loss_work(mf_ctx *ctx, const mf_predictor *pred, int64_t count);

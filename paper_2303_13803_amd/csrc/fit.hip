@@ -15,8 +15,9 @@
 // the rate of the float32 ones (2300 and 152 TFLOP/s measured).  fp16's range is seen to by scaling each operand with a power of two
 // from a bound on it that is never exceeded, to below 2^14; what is within 2^-17 of the bound keeps all its 22 bits, smaller
 // values lose absolute precision of 2^-39 of the bound.  The bounds: a normalised row has |u|_2 <= sqrt(F), so |z1_k| <= |W1_k|_2
-// sqrt(2F) + |b1_k|; |dz3| <= (1 + max |t|) / 2; and through W3 and W2 by their largest values and columns' sums.  Rows of weights have a scale
-// each, of their own largest value.
+// sqrt(2F) + |b1_k|; |dz3| <= (1 + max |t|) / 2; and through W3 and W2 by their largest values and columns' sums.  Features that no norm
+// bounds are looked for; where one is above FIT_LARGEST all of it is done once more in float32 products (wide_kernel), so that what others keep does not
+// depend on it.
 //
 // A workgroup takes FIT_ROWS samples at a time.  Half of its wavefronts ("forward", 32 hidden units each) take them through the layers and back;
 // activations pass between them through LDS.  The others ("sums") add up the gradients of weights, in accumulators that stay until there are no
@@ -122,13 +123,6 @@ __device__ __forceinline__ int afresh(int place)
     return place;
 }
 
-__device__ __forceinline__ float wave_max(float v)
-{
-#pragma unroll
-    for (int off = 32; off >= 1; off >>= 1) v = fmaxf(v, __shfl_xor(v, off));
-    return v;
-}
-
 // Waits for what this wavefront has put into or read from LDS, and for the other wavefronts to have come here, but not for loads and stores of
 // global memory on their way: features are fetched a stage before they are looked at.
 __device__ __forceinline__ void meet()
@@ -156,12 +150,13 @@ struct FitShared {
     float most[10][2 * UB];
 };
 
-// For predictors of many features (wide): layer 1 with the norm's weight and bias folded in, its rows padded with zeros, a wavefront for each
-// hidden unit.  Else the largest feature, where nothing else bounds those that a fit sees: of a predictor without a norm all of them, of one
-// with an SM share those it is made of; of all workloads or those that the samples name, whichever are fewer.
+// Before the pass over the samples, where there is more to know than a workgroup of that pass finds by itself.  Layer 1 as fit_wide.hip takes it: with the
+// norm's weight and bias folded in, its rows padded with zeros, a wavefront for each hidden unit.  And in the last `parts` workgroups the largest
+// feature, where no norm bounds it: of a predictor without a norm, or of an SM share's two; of all workloads or those that the samples name,
+// whichever are fewer.
 struct FoldArgs {
     const float *W1, *b1, *g, *beta;
-    int F, padded, wide;
+    int F, padded, half, rows_of_weights;
     float *W, *bias, *ranges;                               // [H][padded], [H]; [parts]
     const float *X[2];
     const int32_t *index[2];
@@ -172,9 +167,10 @@ struct FoldArgs {
 __global__ __launch_bounds__(256) void fold_kernel(FoldArgs a)
 {
     const int lane = threadIdx.x & 63;
-    if (!a.wide) {
+    if ((int)blockIdx.x >= a.rows_of_weights / 4) {
         __shared__ float most[4];
-        const long long first = (long long)blockIdx.x * 256 + threadIdx.x, step = (long long)a.parts * 256;
+        const int part = blockIdx.x - a.rows_of_weights / 4;
+        const long long first = (long long)part * 256 + threadIdx.x, step = (long long)a.parts * 256;
         float x = 0.0f;
         for (int k = 0; k < 2; ++k) {
             const float *X = (k ? a.X[1] : a.X[0]) + (k ? a.first[1] : a.first[0]);
@@ -193,16 +189,17 @@ __global__ __launch_bounds__(256) void fold_kernel(FoldArgs a)
         x = wave_max(x);
         if (lane == 0) most[threadIdx.x >> 6] = x;
         __syncthreads();
-        if (threadIdx.x == 0) a.ranges[blockIdx.x] = fmaxf(fmaxf(most[0], most[1]), fmaxf(most[2], most[3]));
+        if (threadIdx.x == 0) a.ranges[part] = fmaxf(fmaxf(most[0], most[1]), fmaxf(most[2], most[3]));
         return;
     }
-    const int k = blockIdx.x * 4 + (threadIdx.x >> 6), columns = 2 * a.F;
+    const int k = blockIdx.x * 4 + (threadIdx.x >> 6);
     float sum = 0.0f;
     for (int c = lane; c < a.padded; c += 64) {
+        const int side = c >= a.half, f = c - side * a.half, at = side * a.F + f;
         float v = 0.0f;
-        if (c < columns) {
-            v = a.W1[(size_t)k * columns + c];
-            if (a.g) { sum = fmaf(v, a.beta[c], sum); v *= a.g[c]; }
+        if (f < a.F) {
+            v = a.W1[(size_t)k * 2 * a.F + at];
+            if (a.g) { sum = fmaf(v, a.beta[at], sum); v *= a.g[at]; }
         }
         a.W[(size_t)k * a.padded + c] = v;
     }
@@ -291,7 +288,7 @@ __global__ __launch_bounds__(H * 4, 2) void fit_kernel(const FitArgs a, const fl
     // ---- bounds, and the scales that follow.  Weights are read as the operands that the forward wavefronts make of them: layer 1's with the
     // norm's weight, W2's transpose (or, without a way back, W2), a unit's in two lanes.
     float w[KB][8], u1[XB][8], bias1 = 0.0f, poison = 0.0f;
-    // largest of: targets, features, output weights of either unit, weights of layers 2 and 1, columns' sums of W2, z1 without features and for each
+    // largest of: targets, features (or, of those that a norm bounds, SM shares), output weights of either unit, weights of layers 2 and 1, columns' sums of W2, z1 without features and for each
     float v[9] = {0.0f, 0.0f, 0.0f, 0.0f, 0.0f, 0.0f, 0.0f, 0.0f, 0.0f};
     const float length = sqrtf((float)a.F);
     const auto read_w2 = [&](const int b, float (&to)[8]) {
@@ -364,6 +361,15 @@ __global__ __launch_bounds__(H * 4, 2) void fit_kernel(const FitArgs a, const fl
         poison += a.b2[tid] * 0.0f;
     }
     if (tid < parts) v[1] = ranges[tid];
+    if (!GRAD && EXTRA && with_share && parts == 0)         // nothing else bounds the share: this workgroup's own
+#pragma unroll 4
+        for (int it = tid / T; it < mine; it += H * 4 / T) {
+            const long long s = tile_of(it) * T + tid % T, at = s < a.count ? s : a.count - 1;
+            const int i = a.index[0][at], j = a.index[1][at];
+            const float on = a.X[0][((unsigned)i < (unsigned)a.rows[0] ? i : 0) * a.F + a.sm_feature[0]], off = a.X[1][((unsigned)j < (unsigned)a.rows[1] ? j : 0) * a.F + a.sm_feature[1]];
+            const float share = fabsf(fminf(1.0f - on, off));
+            if (share < INFINITY) v[1] = fmaxf(v[1], share);
+        }
     if (GRAD)                                               // this workgroup's own targets
 #pragma unroll 4
         for (int it = tid / T; it < mine; it += H * 4 / T) {
@@ -916,7 +922,7 @@ int run_fit(mf_ctx *ctx, const mf_predictor *p, const float *d_on, int n, const 
     a.target[0] = s->d_target; a.target[1] = s->d_target_slow;
     a.sigma[0] = d_sigma; a.sigma[1] = d_sigma_slow;
     a.count = s->count;
-    a.W1 = f.wide ? ctx->fit_W1 : p->d_W1; a.b1 = f.wide ? ctx->fit_W1 + FOLD_BIAS : p->d_b1;
+    a.W1 = p->d_W1; a.b1 = p->d_b1;
     a.g = p->d_ln_w; a.beta = p->d_ln_b;
     a.W2 = p->d_W2; a.b2 = p->d_b2;
     a.W3[0] = p->d_W3; a.W3[1] = p->d_W3_slow;
@@ -928,22 +934,31 @@ int run_fit(mf_ctx *ctx, const mf_predictor *p, const float *d_on, int n, const 
     if (a.drop) { a.rule = *rule; a.step = (const unsigned long long *)d_step; }
     a.partial = (float *)d_work;
     a.partial_step = f.step(g != nullptr);
-    const bool bounded = a.norm && !a.W1sm;                 // (a norm bounds what it gives)
-    if (f.wide || !bounded) {
+    float *const ranges = ctx->fit_W1 + FOLD_RANGES;
+    FitArgs folded = a;                                     // as wide_kernel takes it
+    // A workgroup of predictions looks up the SM shares of up to 2048 samples by itself; for more the launch before is no dearer (without and with it, 32 features
+    // and 128 units: 2000 pairs 13 and 18 us, 300,000 91 and 96, a million 261 and 260, three 760 and 736).  With gradients the launch stays: the code for
+    // it, never run, made the loss of a million samples 505 -> 539 us, by what the compiler then keeps in registers of the loop over samples.
+    const bool share_first = a.norm && a.W1sm && (g || a.count > 2048ll * f.grid), fallback = !f.wide && !a.norm, look = !f.wide && (!a.norm || share_first);
+    if (f.wide || look) {
         FoldArgs w{};
         w.W1 = p->d_W1; w.b1 = p->d_b1; w.g = p->d_ln_w; w.beta = p->d_ln_b;
-        w.F = p->F; w.padded = f.padded; w.wide = f.wide;
-        w.W = ctx->fit_W1; w.bias = ctx->fit_W1 + FOLD_BIAS; w.ranges = ctx->fit_W1 + FOLD_RANGES;
+        w.F = p->F; w.padded = f.padded; w.half = f.half; w.rows_of_weights = f.wide || fallback ? f.H : 0;
+        w.W = ctx->fit_W1; w.bias = ctx->fit_W1 + FOLD_BIAS; w.ranges = ranges;
         w.width = a.norm ? 1 : p->F;
         for (int k = 0; k < 2; ++k) { w.X[k] = a.X[k]; w.index[k] = a.index[k]; w.rows[k] = a.rows[k]; w.first[k] = a.norm ? a.sm_feature[k] : 0; }
         w.count = a.count;
         w.listed = 2 * s->count < (long long)n + m;
         const long long values = w.width * (w.listed ? 2 * a.count : (long long)n + m), parts = (values + 2047) / 2048;      // eight values a thread
-        f.parts = w.parts = f.wide ? 0 : (int)(parts < 1 ? 1 : parts < FIT_RANGE_PARTS ? parts : FIT_RANGE_PARTS);
-        hipLaunchKernelGGL(fold_kernel, dim3(f.wide ? f.H / 4 : w.parts), dim3(256), 0, ctx->stream, w);
+        f.parts = w.parts = look ? (int)(parts < 1 ? 1 : parts < FIT_RANGE_PARTS ? parts : FIT_RANGE_PARTS) : 0;
+        hipLaunchKernelGGL(fold_kernel, dim3(w.rows_of_weights / 4 + w.parts), dim3(256), 0, ctx->stream, w);
         MF_HIP(hipGetLastError());
+        folded.W1 = w.W;
+        folded.b1 = w.bias;
     }
-    const int rc = f.wide ? mf_launch_wide(ctx, a, f, g != nullptr) : f.H == 64 ? launch_fit_for<64>(ctx, a, f, g != nullptr) : launch_fit_for<128>(ctx, a, f, g != nullptr);
+    int rc = MF_OK;
+    if (!f.wide) rc = f.H == 64 ? launch_fit_for<64>(ctx, a, f, g != nullptr) : launch_fit_for<128>(ctx, a, f, g != nullptr);
+    if (rc == MF_OK && (f.wide || fallback)) rc = mf_launch_wide(ctx, folded, f, ranges, g != nullptr);
     if (rc != MF_OK || !a.partial) return rc;
     FitOut o{};
     if (g) {

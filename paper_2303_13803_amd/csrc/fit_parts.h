@@ -8,6 +8,9 @@
 typedef float floatx16 __attribute__((ext_vector_type(16)));
 
 constexpr int FIT_WIDE_FROM = 65;                           // features a workload from which on fit_wide.hip takes over
+// Features of a predictor without a norm go to fp16 pieces up to this size: what one of them may be, all samples of a call are scaled by, and the
+// bits that are left for a z1 of about 1 are then still those of float32.
+constexpr float FIT_LARGEST = 4096.0f;
 constexpr int FIT_RANGE_PARTS = 256;                        // workgroups that look for the largest feature, at most
 
 struct FitArgs {
@@ -44,13 +47,20 @@ struct FitPlan {
 };
 
 void mf_plan_wide(const mf_ctx *ctx, long long count, FitPlan *f);
-int mf_launch_wide(mf_ctx *ctx, const FitArgs &a, const FitPlan &f, bool grad);
+int mf_launch_wide(mf_ctx *ctx, const FitArgs &a, const FitPlan &f, const float *ranges, bool grad);     // ranges: f.parts of them
 
 namespace {
 
 // Row r of a 32-row tile of matrix results lies in lane half (r >> 2) & 1; read as unit tile_unit(r), what a lane holds of
 // a tile are the units 8 half .. 8 half + 7 and 16 + 8 half .. 16 + 8 half + 7: eight that share a counter.
 __device__ __forceinline__ int tile_unit(int r) { return (r & 0x13) | (r & 4) << 1 | (r & 8) >> 1; }
+
+__device__ __forceinline__ float wave_max(float v)
+{
+#pragma unroll
+    for (int off = 32; off >= 1; off >>= 1) v = fmaxf(v, __shfl_xor(v, off));
+    return v;
+}
 
 __device__ __forceinline__ float both_halves(float v)
 {

@@ -1,6 +1,6 @@
-// The pass over the samples of a predictor of many features (65 to 256 a workload), in float32 products: features are staged 64 columns at a time, twice a
-// sample, and gradients of layer 1 are kept for 256 columns at a time, which is as many as there are accumulators for: more take another pass over
-// the samples each.  See fit.hip for what is computed.
+// The pass over the samples in float32 products: of predictors of many features (65 to 256 a workload), and of those without a norm where a feature is
+// too large for pieces (FIT_LARGEST).  Features are staged 64 columns at a time, twice a sample, and gradients of layer 1 are kept for 256 columns at a
+// time, which is as many as there are accumulators for: more take another pass over the samples each.  See fit.hip for what is computed.
 #include "fit_parts.h"
 
 namespace {
@@ -18,8 +18,13 @@ constexpr size_t wide_lds_bytes(bool grad)
 }
 
 template <int H, int GT, bool GRAD>
-__global__ __launch_bounds__(H * 4) void wide_kernel(const FitArgs a)
+__global__ __launch_bounds__(H * 4) void wide_kernel(const FitArgs a, const float *__restrict__ ranges, const int parts)
 {
+    if (parts > 0) {                                        // where nothing is too large fit_kernel's results stay, else all of them are written again
+        float most = 0.0f;
+        for (int k = threadIdx.x & 63; k < parts; k += 64) most = fmaxf(most, ranges[k]);
+        if (!(wave_max(most) > FIT_LARGEST)) return;
+    }
     constexpr int T = FIT_ROWS, PITCH = H + 4, XP = FIT_CHUNK + 4, UB = H / 32, THREADS = H * 4, QUADS = H / 8;
     using S = FitSums<H>;
     extern __shared__ __align__(16) float lds[];
@@ -65,21 +70,21 @@ __global__ __launch_bounds__(H * 4) void wide_kernel(const FitArgs a)
     constexpr int EACH_FEATURE = T * FIT_CHUNK / THREADS;
     float feature[EACH_FEATURE];
     auto fetch = [&](const int chunk) {
-        const int c = chunk * FIT_CHUNK + tid % FIT_CHUNK, side = c >= a.F;
-        const float *X = side ? a.X[1] + (c - a.F) : a.X[0] + c;
+        const int c = chunk * FIT_CHUNK + tid % FIT_CHUNK, side = c >= a.half, f = c - side * a.half;
+        const float *X = (side ? a.X[1] : a.X[0]) + f;
 #pragma unroll
         for (int k = 0; k < EACH_FEATURE; ++k) {
             const int s = tid / FIT_CHUNK + k * (THREADS / FIT_CHUNK), at = side ? at_off[s] : at_on[s];
-            feature[k] = c < a.columns && at >= 0 ? X[(size_t)at * a.F] : 0.0f;
+            feature[k] = f < a.F && at >= 0 ? X[(size_t)at * a.F] : 0.0f;
         }
     };
     auto lay = [&](const int chunk) {
-        const int c = chunk * FIT_CHUNK + tid % FIT_CHUNK, side = c >= a.F;
+        const int c = chunk * FIT_CHUNK + tid % FIT_CHUNK, side = c >= a.half, f = c - side * a.half;
 #pragma unroll
         for (int k = 0; k < EACH_FEATURE; ++k) {
             const int s = tid / FIT_CHUNK + k * (THREADS / FIT_CHUNK);
             const float2 m = moments[2 * s + side];
-            xs[s * XP + tid % FIT_CHUNK] = c < a.columns && at_on[s] >= 0 ? (feature[k] - m.x) * m.y : 0.0f;
+            xs[s * XP + tid % FIT_CHUNK] = f < a.F && at_on[s] >= 0 ? (feature[k] - m.x) * m.y : 0.0f;
         }
     };
     // bias, ReLU and dropout of this lane's 16 units of one layer
@@ -334,14 +339,14 @@ __global__ __launch_bounds__(H * 4) void wide_kernel(const FitArgs a)
 }
 
 template <int H, int GT, bool GRAD>
-int launch_wide(mf_ctx *ctx, const FitArgs &a, const FitPlan &f)
+int launch_wide(mf_ctx *ctx, const FitArgs &a, const FitPlan &f, const float *ranges)
 {
     const unsigned flag = 1u << (21 + (H == 128 ? 2 : 0) + (GRAD ? 1 : 0));
     if (!(ctx->kernels_configured & flag)) {
         MF_HIP(hipFuncSetAttribute((const void *)wide_kernel<H, GT, GRAD>, hipFuncAttributeMaxDynamicSharedMemorySize, (int)wide_lds_bytes<H>(GRAD)));
         ctx->kernels_configured |= flag;
     }
-    hipLaunchKernelGGL((wide_kernel<H, GT, GRAD>), dim3(f.grid, GRAD ? f.passes : 1), dim3(H * 4), wide_lds_bytes<H>(GRAD), ctx->stream, a);
+    hipLaunchKernelGGL((wide_kernel<H, GT, GRAD>), dim3(f.grid, GRAD ? f.passes : 1), dim3(H * 4), wide_lds_bytes<H>(GRAD), ctx->stream, a, ranges, f.parts);
     MF_HIP(hipGetLastError());
     return MF_OK;
 }
@@ -361,9 +366,9 @@ void mf_plan_wide(const mf_ctx *ctx, long long count, FitPlan *f)
     f->grid = (int)(tiles < units ? tiles : units);
 }
 
-int mf_launch_wide(mf_ctx *ctx, const FitArgs &a, const FitPlan &f, bool grad)
+int mf_launch_wide(mf_ctx *ctx, const FitArgs &a, const FitPlan &f, const float *ranges, bool grad)
 {
-    if (f.H == 64) return grad ? launch_wide<64, FIT_WIDE_TILES, true>(ctx, a, f) : launch_wide<64, 1, false>(ctx, a, f);
-    return grad ? launch_wide<128, FIT_WIDE_TILES, true>(ctx, a, f) : launch_wide<128, 1, false>(ctx, a, f);
+    if (f.H == 64) return grad ? launch_wide<64, FIT_WIDE_TILES, true>(ctx, a, f, ranges) : launch_wide<64, 1, false>(ctx, a, f, ranges);
+    return grad ? launch_wide<128, FIT_WIDE_TILES, true>(ctx, a, f, ranges) : launch_wide<128, 1, false>(ctx, a, f, ranges);
 }
 

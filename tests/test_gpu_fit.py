@@ -177,6 +177,105 @@ def test_features_of_a_thousand_scales(ctx):
     compare(call(ctx, s), definition(s))
 
 
+@pytest.mark.parametrize("H", [64, 128])
+@pytest.mark.parametrize("F", [1, 2, 7, 49, 63, 255])
+def test_by_odd_features_without_an_sm_share(ctx, F, H):
+    s = problem(F + H, 97, F, H, norm=F % 3 > 0, missing=True)
+    compare(call(ctx, s, (0.25, 9, 9)), definition(s, (0.25, 9, 9)))
+
+
+@pytest.mark.parametrize("H", [64, 128])
+@pytest.mark.parametrize("F", [5, 40])
+@pytest.mark.parametrize("largest", [100.0, 4096.0, 4097.0, 1e7, 1e12])
+@pytest.mark.parametrize("drop", [None, (0.2, 3, 3)])
+def test_a_few_large_features_without_a_norm(ctx, F, H, largest, drop):
+    """Beside features of about 1, which keep their precision; with weights that make something of both."""
+    s = problem(30, 210, F, H, norm=False)
+    s["x_on"][:3, 2] = largest
+    s["params"]["W1"][:, 2] /= np.float32(largest)
+    compare(call(ctx, s, drop), definition(s, drop))
+    sigma = torch.full((210,), 7.0, device="cuda")
+    ctx.predict_pairs(predictor(ctx, s), dev(s["x_on"]), dev(s["x_off"]), dev(s["on"]), dev(s["off"]), sigma)
+    ref.within(sigma.cpu().numpy(), *definition(s)["sigma"], "sigma")
+
+
+@pytest.mark.parametrize("norm", [False, True])
+@pytest.mark.parametrize("largest", [100.0, 1e7])
+def test_a_large_sm_share(ctx, largest, norm):
+    s = problem(31, 210, 8, 64, norm=norm, sm=True, slow=True)
+    s["x_on"][:3, SM[0]], s["x_off"][:3, SM[1]] = -largest, largest
+    s["params"]["W1sm"] /= np.float32(largest)
+    compare(call(ctx, s, (0.2, 3, 3)), definition(s, (0.2, 3, 3)))
+
+
+@pytest.mark.parametrize("norm", [False, True])
+def test_many_predictions_of_the_same_pairs(ctx, norm):
+    """More than a workgroup looks up by itself; every pair of 50 and 40 workloads again and again."""
+    s = problem(38, 2000, 8, 128, norm=norm, sm=True)
+    s["on"], s["off"] = np.repeat(np.arange(50), 40).astype(np.int32), np.tile(np.arange(40), 50).astype(np.int32)
+    which = np.random.default_rng(38).integers(0, 2000, 700001)
+    sigma = torch.full((700001,), 7.0, device="cuda")
+    ctx.predict_pairs(predictor(ctx, s), dev(s["x_on"]), dev(s["x_off"]), dev(s["on"][which]), dev(s["off"][which]), sigma)
+    value, bound = definition(s)["sigma"]
+    ref.within(sigma.cpu().numpy(), value[which], bound[which], "sigma")
+
+
+def test_large_features_that_no_sample_names(ctx):
+    """Whether they are looked at or not (few samples, many samples): predictions of the others do not change beyond their bounds."""
+    for count in (20, 2000):
+        s = problem(32, count, 16, 128, norm=False)
+        s["x_on"][7], s["x_off"][9] = 1e20, np.inf
+        s["on"][s["on"] == 7], s["off"][s["off"] == 9] = 8, 8
+        compare(call(ctx, s), definition(s))
+
+
+@pytest.mark.parametrize("H", [64, 128])
+def test_targets_far_from_what_a_logistic_gives(ctx, H):
+    s = problem(33, 500, 16, H, slow=True)
+    s["target"] = (s["target"] * 60 - 10).astype(np.float32)
+    s["target_slow"][::50] = -40.0
+    compare(call(ctx, s, (0.1, 4, 4)), definition(s, (0.1, 4, 4)))
+
+
+@pytest.mark.parametrize("p", [2.0 ** -16, 0.99, 65535 / 65536])
+def test_hardly_any_dropout_and_hardly_anything_left(ctx, p):
+    s = problem(34, 400, 16, 128)
+    compare(call(ctx, s, (p, 4, 4)), definition(s, (p, 4, 4)))
+
+
+def test_weights_that_are_all_zero(ctx):
+    s = problem(35, 100, 16, 64)
+    for k in s["params"]:
+        s["params"][k][:] = 0.0
+    compare(call(ctx, s), definition(s))
+
+
+@pytest.mark.parametrize("F", [16, 100])
+@pytest.mark.parametrize("norm", [False, True])
+@pytest.mark.parametrize("value", [np.nan, np.inf, -np.inf])
+def test_a_feature_that_is_not_finite_shows_where_it_is_used(ctx, F, norm, value):
+    s = problem(36, 300, F, 64, norm=norm)
+    s["x_off"][5, 3] = value
+    s["off"][:10] = 5
+    got = call(ctx, s)
+    used = s["off"] == 5
+    assert np.isnan(got["loss"]).all() and np.isfinite(got["sigma"][~used]).all()
+    if norm or np.isnan(value):
+        assert np.isnan(got["sigma"][used]).all()
+    else:                                                   # (without a norm it may also make the logistic certain)
+        assert (np.isnan(got["sigma"][used]) | (got["sigma"][used] == 0) | (got["sigma"][used] == 1)).all()
+
+
+def test_predictions_without_workloads(ctx):
+    s = problem(37, 70, 8, 64, slow=True)
+    pred = predictor(ctx, s)
+    none = torch.empty((0, 8), device="cuda")
+    for x_on, x_off in ((none, dev(s["x_off"])), (dev(s["x_on"]), none), (none, none)):
+        sigma, slow = (torch.full((70,), 7.0, device="cuda") for _ in range(2))
+        ctx.predict_pairs(pred, x_on, x_off, dev(s["on"]), dev(s["off"]), sigma, slow)
+        assert (sigma == 0).all() and (slow == 0).all()
+
+
 def test_a_fit_that_has_diverged_shows(ctx):
     s = problem(20, 100, 8, 64)
     s["params"]["W1"][3, 2] = np.nan
