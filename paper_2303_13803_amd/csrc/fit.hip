@@ -737,9 +737,11 @@ __global__ __launch_bounds__(H * 4, 2) void fit_kernel(const FitArgs a, const fl
         if (scout && it + 2 < mine) name(it + 2, looked);
         if (GRAD && it > 0) add_w1(it - 1, [] {});
         draw_next(1)();
+        // (features are read right after the last meeting of all)
+        if (!GRAD && more) stage(it + 1);
         meet();
         draw_next(2)();
-        if (more) stage(it + 1);
+        if (GRAD && more) stage(it + 1);
         if (it + 2 < mine) fetch(it + 2, 0);
         if (!GRAD) {
             draw_next(3)();
