@@ -276,18 +276,6 @@ def test_predictions_without_workloads(ctx):
         assert (sigma == 0).all() and (slow == 0).all()
 
 
-@pytest.mark.parametrize("norm", [False, True])
-def test_many_predictions_of_the_same_pairs(ctx, norm):
-    """More than a workgroup looks up by itself; every pair of 50 and 40 workloads again and again."""
-    s = problem(38, 2000, 8, 128, norm=norm, sm=True)
-    s["on"], s["off"] = np.repeat(np.arange(50), 40).astype(np.int32), np.tile(np.arange(40), 50).astype(np.int32)
-    which = np.random.default_rng(38).integers(0, 2000, 700001)
-    sigma = torch.full((700001,), 7.0, device="cuda")
-    ctx.predict_pairs(predictor(ctx, s), dev(s["x_on"]), dev(s["x_off"]), dev(s["on"][which]), dev(s["off"][which]), sigma)
-    value, bound = definition(s)["sigma"]
-    ref.within(sigma.cpu().numpy(), value[which], bound[which], "sigma")
-
-
 def test_a_fit_that_has_diverged_shows(ctx):
     s = problem(20, 100, 8, 64)
     s["params"]["W1"][3, 2] = np.nan
