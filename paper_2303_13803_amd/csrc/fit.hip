@@ -467,8 +467,7 @@ __global__ __launch_bounds__(H * 4, 2) void fit_kernel(const FitArgs a, const fl
         const auto operand = [&](auto *rows, const int place, const int b) { return Frag{rows[0].chunk(place ^ b << 5), rows[1].chunk(place ^ b << 5)}; };
         // a unit's value after ReLU and dropout: its bit, as a mask
         const auto kept = [](const float z, const unsigned keep, const int e) {
-            const int bit = e >> 1 | (e & 1) << 2;
-            return __uint_as_float(__float_as_uint(fmaxf(z, 0.0f)) & (unsigned)((int)(keep << (31 - bit)) >> 31));
+            return __uint_as_float(__float_as_uint(fmaxf(z, 0.0f)) & (unsigned)__builtin_amdgcn_sbfe((int)keep, e >> 1 | (e & 1) << 2, 1));
         };
         const floatx16 zero = {0};
         meet();                                             // the first samples are there
@@ -596,26 +595,29 @@ __global__ __launch_bounds__(H * 4, 2) void fit_kernel(const FitArgs a, const fl
     }
 
     // ---- sums, and what is to come
+    const float inverse = 1.0f / (float)a.F;
     const auto stage = [&](const int it) {                  // what has been fetched, normalised, as pieces
         const int to = it & 1;
-        float sum = 0.0f, mean = 0.0f, by = s_x;
+        float sum = 0.0f, mean = 0.0f, by = s_x, v[EACH];
+        _Float16 hi[EACH], lo[EACH];
 #pragma unroll
-        for (int e = 0; e < EACH; ++e) sum += sub * EACH + e < a.F ? x[e / 4][e % 4] : 0.0f;
+        for (int e = 0; e < EACH; ++e) {
+            v[e] = sub * EACH + e < a.F && next_real ? x[e / 4][e % 4] : 0.0f;
+            sum += v[e];
+        }
         sum = group_sum<UB>(sum);
         if (a.norm) {
             float squares = 0.0f;
-            mean = sum / (float)a.F;
+            mean = sum * inverse;
 #pragma unroll
             for (int e = 0; e < EACH; ++e) {
-                const float d = sub * EACH + e < a.F ? x[e / 4][e % 4] - mean : 0.0f;
-                squares = fmaf(d, d, squares);
+                v[e] = sub * EACH + e < a.F ? v[e] - mean : 0.0f;
+                squares = fmaf(v[e], v[e], squares);
             }
-            by = s_x / sqrtf(group_sum<UB>(squares) / (float)a.F + a.eps);
+            by = s_x * __builtin_amdgcn_rsqf(fmaf(group_sum<UB>(squares), inverse, a.eps));     // (to a step of float32)
         }
-        float v[EACH];
-        _Float16 hi[EACH], lo[EACH];
 #pragma unroll
-        for (int e = 0; e < EACH; ++e) v[e] = sub * EACH + e < a.F && next_real ? (x[e / 4][e % 4] - mean) * by : 0.0f;
+        for (int e = 0; e < EACH; ++e) v[e] *= by;
         split(v, hi, lo, minus_one);
 #pragma unroll
         for (int e = 0; e < EACH; e += 4) {
@@ -624,7 +626,7 @@ __global__ __launch_bounds__(H * 4, 2) void fit_kernel(const FitArgs a, const fl
             *(half4v *)((char *)&sh.xs[to][0] + place) = half4v{hi[e], hi[e + 1], hi[e + 2], hi[e + 3]};
             *(half4v *)((char *)&sh.xs[to][1] + place) = half4v{lo[e], lo[e + 1], lo[e + 2], lo[e + 3]};
         }
-        if (sub == 0) sh.bad[to][side][own] = next_real ? sum * 0.0f : 0.0f;
+        if (sub == 0) sh.bad[to][side][own] = sum * 0.0f;
     };
     const unsigned short limit = (unsigned short)(rule.limit - 1);      // (a dropout's limit is at least 1)
     const ushort2v below = {limit, limit};
@@ -637,8 +639,9 @@ __global__ __launch_bounds__(H * 4, 2) void fit_kernel(const FitArgs a, const fl
         unsigned keep = 0;
 #pragma unroll
         for (int w = 0; w < 4; ++w) {
-            const ushort2v above = __builtin_elementwise_min(__builtin_elementwise_sub_sat(__builtin_bit_cast(ushort2v, bits.w[w]), below), ushort2v{1, 1});
-            keep |= __builtin_bit_cast(unsigned, above) << w;
+            unsigned above = __builtin_bit_cast(unsigned, __builtin_elementwise_sub_sat(__builtin_bit_cast(ushort2v, bits.w[w]), below));
+            asm volatile("" : "+v"(above));                 // no instruction (and no comparison of either half in the place of two instructions for both)
+            keep |= __builtin_bit_cast(unsigned, __builtin_elementwise_min(__builtin_bit_cast(ushort2v, above), ushort2v{1, 1})) << w;
         }
         sh.keep[it & 1][layer][s][k] = (unsigned char)(keep | keep >> 12);
     };
@@ -697,13 +700,12 @@ __global__ __launch_bounds__(H * 4, 2) void fit_kernel(const FitArgs a, const fl
         for (int b = 0; b < 2; ++b) {
             products(d[b], u[b], gw1);
 #pragma unroll
-            for (int e = 0; e < 8; ++e) gb1 = __builtin_fmaf((float)d[b].hi[e], one, __builtin_fmaf((float)d[b].lo[e], one, gb1));
-            if (EXTRA)
-#pragma unroll
-                for (int e = 0; e < 8; ++e) {
-                    const float by = sh.share[it & 3][16 * b + 8 * hh + e];
-                    gsm = __builtin_fmaf((float)d[b].hi[e], by, __builtin_fmaf((float)d[b].lo[e], by, gsm));
-                }
+            for (int e = 0; e < 8; ++e) {
+                if (!EXTRA) { gb1 = __builtin_fmaf((float)d[b].hi[e], one, __builtin_fmaf((float)d[b].lo[e], one, gb1)); continue; }
+                const float v = __builtin_fmaf((float)d[b].hi[e], one, (float)d[b].lo[e]);
+                gb1 += v;
+                gsm = fmaf(v, sh.share[it & 3][16 * b + 8 * hh + e], gsm);
+            }
         }
     };
     const auto add_w2 = [&](const int of, const int b, const auto &meanwhile) {      // half of a tile's samples
