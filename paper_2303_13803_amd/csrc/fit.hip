@@ -936,6 +936,9 @@ int run_fit(mf_ctx *ctx, const mf_predictor *p, const float *d_on, int n, const 
     a.sm_feature[0] = p->sm_on_feature; a.sm_feature[1] = p->sm_off_feature;
     a.drop = rule && rule->limit > 0;
     if (a.drop) { a.rule = *rule; a.step = (const unsigned long long *)d_step; }
+    // Predictions that the device holds at once, a workgroup each (2048 threads a compute unit, 4 H a pair), without staging and looking for bounds: one of 32 features and
+    // 128 units 3.5 us, with them 10.6; 1024 8.3 and 10.9; 2048 14.2 and 11.0.  With 16 and 64: 3.1 and 7.5; 2048 6.5 and 7.9; 4096 10.3 and 7.9.
+    if (!d_work && a.count <= (ctx->n_cus > 0 ? ctx->n_cus : 256) * (512ll / f.H)) return mf_launch_few(ctx, a, f.H);
     a.partial = (float *)d_work;
     a.partial_step = f.step(g != nullptr);
     float *const ranges = ctx->fit_W1 + FOLD_RANGES;

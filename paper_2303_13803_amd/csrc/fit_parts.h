@@ -46,6 +46,7 @@ struct FitPlan {
     long long step(bool grad) const { return (values(grad) + 15) & ~15; }
 };
 
+int mf_launch_few(mf_ctx *ctx, const FitArgs &a, int H);    // predictions, without dropout and loss: a.count of them
 void mf_plan_wide(const mf_ctx *ctx, long long count, FitPlan *f);
 int mf_launch_wide(mf_ctx *ctx, const FitArgs &a, const FitPlan &f, const float *ranges, bool grad);     // ranges: f.parts of them
 

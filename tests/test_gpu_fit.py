@@ -320,6 +320,34 @@ def test_predictions_of_listed_pairs(ctx, count, F, H):
     assert torch.equal(only, sigma)
 
 
+@pytest.mark.parametrize("count, H", [(1024, 128), (1025, 128), (2048, 64), (2049, 64)])
+def test_predictions_about_as_many_as_the_device_holds(ctx, count, H):
+    s = problem(count, count, 12, H, n=300, m=200, sm=True, slow=True, missing=True)
+    sigma, slow = (torch.full((count,), 7.0, device="cuda") for _ in range(2))
+    ctx.predict_pairs(predictor(ctx, s), dev(s["x_on"]), dev(s["x_off"]), dev(s["on"]), dev(s["off"]), sigma, slow)
+    expected = definition(s)
+    for got, name in ((sigma, "sigma"), (slow, "sigma_slow")):
+        ref.within(got.cpu().numpy(), *expected[name], name)
+
+
+@pytest.mark.parametrize("H", [64, 128])
+@pytest.mark.parametrize("norm", [False, True])
+@pytest.mark.parametrize("F", [1, 2, 5, 6, 63, 64, 65, 130, 255])
+def test_single_predictions_by_features(ctx, F, norm, H):
+    """A few pairs, an infinity and a NaN among their features."""
+    s = problem(40 + F, 9, F, H, norm=norm)
+    s["x_on"][49], s["x_off"][39, F - 1] = np.nan, np.inf
+    s["on"][:7], s["off"][:7] = [0, 1, 49, 3, -1, 5, 50], [0, 1, 2, 39, 4, 40, 6]
+    s["on"][7:], s["off"][7:] = 8, 9
+    sigma = torch.full((9,), 7.0, device="cuda")
+    ctx.predict_pairs(predictor(ctx, s), dev(s["x_on"]), dev(s["x_off"]), dev(s["on"]), dev(s["off"]), sigma)
+    got, good = sigma.cpu().numpy(), [0, 1, 4, 5, 6, 7, 8]
+    with np.errstate(invalid="ignore"):
+        value, bound = definition(s)["sigma"]
+    ref.within(got[good], value[good], bound[good], "sigma")
+    assert np.isnan(got[2]) and (np.isnan(got[3]) or not norm and got[3] in (0.0, 1.0)) and (got[4:7] == 0).all()
+
+
 @pytest.mark.parametrize("H", [64, 128])
 @pytest.mark.parametrize("split", [0, 1])
 def test_scores_of_a_predictor_with_a_norm(ctx, H, split):
