@@ -7,7 +7,9 @@
 
 typedef float floatx16 __attribute__((ext_vector_type(16)));
 
-constexpr int FIT_WIDE_FROM = 65;                           // features a workload from which on fit_wide.hip takes over
+// Features a workload from which on fit_wide.hip takes over: as many as fit_kernel has accumulators and LDS for.  With 64, 100,000 samples and 128 units it took
+// 439 us and fit_kernel takes 151; with 64 units 278 and 142.
+constexpr int FIT_WIDE_FROM = 65;
 // Features of a predictor without a norm go to fp16 pieces up to this size: what one of them may be, all samples of a call are scaled by, and the
 // bits that are left for a z1 of about 1 are then still those of float32.
 constexpr float FIT_LARGEST = 4096.0f;
@@ -20,7 +22,7 @@ struct FitArgs {
     const float *target[2];                                 // throughput, slowdown (null: not trained)
     float *sigma[2];                                        // (null: not wanted)
     long long count;
-    const float *W1, *b1, *g, *beta;                        // wide: layer 1 with the norm folded in (see fold_kernel)
+    const float *W1, *b1, *g, *beta;                        // for fit_wide.hip W1 and b1 with the norm folded in (see fold_kernel)
     const float *W2, *b2, *W3[2], *b3[2], *W1sm;            // ([1] and W1sm may be null)
     int norm, sm_feature[2];
     float eps;
@@ -39,7 +41,7 @@ struct FitSums {
 enum { REST_B3 = 0, REST_B3S, REST_LOSS };
 
 struct FitPlan {
-    int H, columns, padded, half, passes, tiles, grid;      // tiles: of 32 columns that a pass over the samples keeps gradients of, for each wavefront
+    int H, columns, padded, half, passes, tiles, grid;      // tiles: fit_kernel's, of 32 columns; passes: over the samples, fit_wide.hip's
     int parts;                                              // workgroups that look for bounds
     bool wide;
     int values(bool grad) const { return (H == 64 ? FitSums<64>::G : FitSums<128>::G) + (grad ? H * padded : 0); }

@@ -1,6 +1,7 @@
 // Predictions of a few listed pairs (see fit.hip for what is computed), where nothing counts but the time until the answer is there: a workgroup a pair, in float32.
 // Four lanes share a hidden unit.  Nothing is looked for or prepared before, and weights, which do not depend on the pair, are on their way to
-// registers (those of layer 2, and of the first 128 columns of layer 1) before the pair's rows are known.
+// registers (those of layer 2, and of the first 128 columns of layer 1) before the pair's rows are known.  Bound by the latency of two loads that follow one another
+// (indices, features) and four meetings; weights come from L2.  Measured: one pair of 32 features a workload through 128 units 3.5 us, 256 of them 4.2.
 #include "fit_parts.h"
 
 namespace {
