@@ -58,13 +58,6 @@ namespace {
 // a tile are the units 8 half .. 8 half + 7 and 16 + 8 half .. 16 + 8 half + 7: eight that share a counter.
 __device__ __forceinline__ int tile_unit(int r) { return (r & 0x13) | (r & 4) << 1 | (r & 8) >> 1; }
 
-__device__ __forceinline__ float wave_max(float v)
-{
-#pragma unroll
-    for (int off = 32; off >= 1; off >>= 1) v = fmaxf(v, __shfl_xor(v, off));
-    return v;
-}
-
 __device__ __forceinline__ float both_halves(float v)
 {
     const auto s = __builtin_amdgcn_permlane32_swap(__float_as_uint(v), __float_as_uint(v), false, false);
