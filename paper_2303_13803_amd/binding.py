@@ -7,6 +7,7 @@ module raises.
 """
 import ctypes as C
 import os
+import struct
 
 import torch
 
@@ -47,16 +48,20 @@ class Samples(C.Structure):
                 ("count", C.c_int64)]
 
 
-# members of mf_gradients, the names their parameters have in a predictor's dictionary, and their sizes for F features and H hidden units
-PARAMETERS = (("d_W1", "W1", lambda F, H: 2 * F * H), ("d_b1", "b1", lambda F, H: H), ("d_W2", "W2", lambda F, H: H * H),
-              ("d_b2", "b2", lambda F, H: H), ("d_W3", "W3", lambda F, H: H), ("d_b3", "b3", lambda F, H: 1),
-              ("d_W1sm", "W1sm", lambda F, H: H), ("d_W3_slow", "W3slow", lambda F, H: H), ("d_b3_slow", "b3slow", lambda F, H: 1),
-              ("d_ln_w", "ln_w", lambda F, H: 2 * F), ("d_ln_b", "ln_b", lambda F, H: 2 * F))
+# members of mf_gradients, the names their parameters have in a predictor's dictionary, and their sizes: so many times F, H, 1, H * H and F * H
+PARAMETERS = (("d_W1", "W1", (0, 0, 0, 0, 2)), ("d_b1", "b1", (0, 1, 0, 0, 0)), ("d_W2", "W2", (0, 0, 0, 1, 0)),
+              ("d_b2", "b2", (0, 1, 0, 0, 0)), ("d_W3", "W3", (0, 1, 0, 0, 0)), ("d_b3", "b3", (0, 0, 1, 0, 0)),
+              ("d_W1sm", "W1sm", (0, 1, 0, 0, 0)), ("d_W3_slow", "W3slow", (0, 1, 0, 0, 0)), ("d_b3_slow", "b3slow", (0, 0, 1, 0, 0)),
+              ("d_ln_w", "ln_w", (2, 0, 0, 0, 0)), ("d_ln_b", "ln_b", (2, 0, 0, 0, 0)))
 
 
 class Gradients(C.Structure):
     _fields_ = [(member, C.c_void_p) for member, _, _ in PARAMETERS]
 
+
+# The same three as bytes, which take a third of the time to make.
+DROPOUT_RULE, SAMPLES, GRADIENTS = struct.Struct("@fQQP"), struct.Struct("@PPPPq"), struct.Struct("@11P")
+assert (DROPOUT_RULE.size, SAMPLES.size, GRADIENTS.size) == (C.sizeof(DropoutRule), C.sizeof(Samples), C.sizeof(Gradients))
 
 LAYER_TYPES = {torch.float32: 0, torch.float16: 1, torch.bfloat16: 2}
 
@@ -104,14 +109,14 @@ def load_library():
                                             C.POINTER(Result)]
     lib.mf_measure_ceilings.argtypes = [vp, vp, i64, C.POINTER(C.c_float * 8)]
     pred, f32 = C.POINTER(Predictor), C.c_float
-    lib.mf_predictor_loss.argtypes = [vp, pred, vp, i32, vp, i32, C.POINTER(Samples), C.POINTER(DropoutRule), f32,
-                                      C.POINTER(Gradients), vp, vp, vp, vp, i64]
+    lib.mf_predictor_loss.argtypes = [vp, pred, vp, i32, vp, i32, vp, vp, f32,
+                                      vp, vp, vp, vp, vp, i64]
     lib.mf_predictor_loss_work.argtypes = [vp, pred, i64]
     lib.mf_predict_pairs.argtypes = [vp, pred, vp, i32, vp, i32, vp, vp, i64, vp, vp]
     lib.mf_layer_norm.argtypes = [vp, i32, vp, i64, i64, i64, vp, vp, f32, vp, i64]
     lib.mf_layer_norm_grad.argtypes = [vp, i32, vp, i64, i64, i64, vp, i64, vp, f32, vp, i64, vp, vp, vp, i64]
     lib.mf_layer_norm_grad_work.argtypes = [vp, i64, i64]
-    lib.mf_dropout.argtypes = [vp, i32, vp, i64, i64, i64, C.POINTER(DropoutRule), i32, vp, i64]
+    lib.mf_dropout.argtypes = [vp, i32, vp, i64, i64, i64, vp, i32, vp, i64]
     lib.mf_set_option.argtypes = [vp, C.c_char_p, i64]
     lib.mf_last_timings.argtypes = [vp, C.POINTER(C.c_float * 16)]
     lib.mf_strerror.argtypes = [i32]
@@ -168,44 +173,48 @@ class Context:
             raise MuxmatchError(rc, detail)
         return rc
 
-    # (Every look at a tensor's attribute is a tenth of a microsecond or more, and the smallest calls are two on the device.)
-    def _flat(self, t, dtype, count, what, optional=False):
+    # Calls of the layers and of fits may be two microseconds on the device, and every look at a tensor's attribute is a tenth of one or more: each is looked
+    # at once, and what is wrong with a tensor is found out after it has been refused.
+    def _flat(self, t, dtype, count, what):
         """Pointer of a contiguous tensor of `count` values on this context's device."""
-        if t is None and optional:
-            return None
         try:
+            if t.dtype is dtype and t.get_device() == self.device and t.is_contiguous() and t.numel() == count:
+                return t.data_ptr()
             fits = t.dtype == dtype and t.get_device() == self.device and t.is_contiguous()
         except AttributeError:
             fits = False
         if not fits:
             raise TypeError(f"{what}: expected a contiguous tensor of {dtype} on device {self.device}")
-        if t.numel() != count:
-            raise ValueError(f"{what}: expected {count} values, got {t.numel()}")
-        return t.data_ptr() or None
+        raise ValueError(f"{what}: expected {count} values, got {t.numel()}")
 
     def _rows(self, t, kind, shape, what):
         """(pointer, pitch) of a matrix of this type and shape whose rows may lie apart but whose values lie side by side."""
         try:
             if t.get_device() != self.device:
                 raise TypeError(f"{what}: expected a tensor on device {self.device}")
-            if t.dtype != kind or t.shape != shape:
+            if t.dtype is not kind or t.shape != shape:
                 raise ValueError(f"{what}: expected a matrix of the input's shape and type")
         except AttributeError:
             raise TypeError(f"{what}: expected a tensor on device {self.device}") from None
+        return t.data_ptr(), self._pitch(t, shape, what)
+
+    def _pitch(self, t, shape, what):
         pitch, step = t.stride()
         rows, width = shape
         if rows < 2:
             pitch = max(width, 1)
         if (step != 1 and width > 1) or pitch < width:
             raise ValueError(f"{what}: the values of a row have to lie side by side, rows must not overlap")
-        return t.data_ptr() or None, pitch
+        return pitch
 
     def _matrix(self, t, what):
-        """Type, its number, and shape of a matrix."""
-        kind = t.dtype if isinstance(t, torch.Tensor) else None
-        if kind not in LAYER_TYPES or t.dim() != 2:
+        """Type, its number, shape, pointer and pitch of a matrix."""
+        if not isinstance(t, torch.Tensor) or t.dtype not in LAYER_TYPES or t.dim() != 2:
             raise TypeError(f"{what}: expected a float32, float16 or bfloat16 matrix")
-        return kind, LAYER_TYPES[kind], t.shape
+        if t.get_device() != self.device:
+            raise TypeError(f"{what}: expected a tensor on device {self.device}")
+        kind, shape = t.dtype, t.shape
+        return kind, LAYER_TYPES[kind], shape, t.data_ptr(), self._pitch(t, shape, what)
 
     def _work(self, work, needed, *args):
         """The caller's scratch (the call itself looks at its size), or needed(*args) bytes from torch's allocator, in the order of this
@@ -218,18 +227,15 @@ class Context:
             raise TypeError(f"work: expected a contiguous tensor of torch.uint8 on device {self.device}")
         return work
 
-    def _dropout(self, p, seed, step):
-        rule = DropoutRule(float(p), int(seed) & (2 ** 64 - 1), 0, None)
+    def _dropout(self, p, seed, step=0):
+        """An mf_dropout_rule."""
         if isinstance(step, torch.Tensor):
-            rule.d_step = self._flat(step, torch.int64, 1, "step")
-        else:
-            rule.step = int(step) & (2 ** 64 - 1)
-        return rule
+            return DROPOUT_RULE.pack(float(p), int(seed) & (2 ** 64 - 1), 0, self._flat(step, torch.int64, 1, "step"))
+        return DROPOUT_RULE.pack(float(p), int(seed) & (2 ** 64 - 1), int(step) & (2 ** 64 - 1), 0)
 
     def layer_norm(self, x, weight, bias, y, eps=1e-5):
         """y = layer norm of the rows of x (float32, float16 or bfloat16; weight and bias float32).  y may be x."""
-        kind, number, shape = self._matrix(x, "x")
-        px, ldx = self._rows(x, kind, shape, "x")
+        kind, number, shape, px, ldx = self._matrix(x, "x")
         py, ldy = self._rows(y, kind, shape, "y")
         rows, width = shape
         self._check(_lib.mf_layer_norm(self._h, number, px, rows, width, ldx,
@@ -245,35 +251,31 @@ class Context:
 
     def layer_norm_grad(self, x, dy, weight, dx, dweight, dbias, eps=1e-5, work=None):
         """dx, dweight and dbias of layer_norm from dy.  dx may be x or dy."""
-        kind, number, shape = self._matrix(x, "x")
-        px, ldx = self._rows(x, kind, shape, "x")
+        kind, number, shape, px, ldx = self._matrix(x, "x")
         pdy, lddy = self._rows(dy, kind, shape, "dy")
         pdx, lddx = self._rows(dx, kind, shape, "dx")
         rows, width = shape
         work = self._work(work, self.layer_norm_grad_work, rows, width)
-        flat = lambda t, what: self._flat(t, torch.float32, width, what)
+        f32 = torch.float32
         self._check(_lib.mf_layer_norm_grad(self._h, number, px, rows, width, ldx, pdy, lddy,
-                                            flat(weight, "weight"), float(eps), pdx, lddx, flat(dweight, "dweight"),
-                                            flat(dbias, "dbias"), work.data_ptr(), work.numel()))
+                                            self._flat(weight, f32, width, "weight"), float(eps), pdx, lddx, self._flat(dweight, f32, width, "dweight"),
+                                            self._flat(dbias, f32, width, "dbias"), work.data_ptr(), work.numel()))
 
     def dropout(self, x, y, p, seed, step=0, layer=0):
         """y = dropout of x, the mask made from (seed, step, layer, element); on a gradient, the backward pass.
         step: a number, or an int64 tensor of one value on the device.  y may be x."""
-        kind, number, shape = self._matrix(x, "x")
-        px, ldx = self._rows(x, kind, shape, "x")
+        kind, number, shape, px, ldx = self._matrix(x, "x")
         py, ldy = self._rows(y, kind, shape, "y")
-        rule = self._dropout(p, seed, step)
         rows, width = shape
-        self._check(_lib.mf_dropout(self._h, number, px, rows, width, ldx, C.byref(rule), int(layer), py, ldy))
+        self._check(_lib.mf_dropout(self._h, number, px, rows, width, ldx, self._dropout(p, seed, step), int(layer), py, ldy))
 
-    def _sides(self, pred, x_on, x_off):
-        """Features of both sides: [n, F] and [m, F]."""
-        out = []
-        for x, what in ((x_on, "x_on"), (x_off, "x_off")):
-            if not isinstance(x, torch.Tensor) or x.dim() != 2 or x.shape[1] != pred.F:
-                raise ValueError(f"{what}: expected a matrix of {pred.F} features a workload")
-            out += [self._flat(x, torch.float32, x.numel(), what), x.shape[0]]
-        return out
+    def _side(self, x, F, what):
+        """Pointer and rows of a side's features, [rows, F]."""
+        shape = x.shape if isinstance(x, torch.Tensor) else ()
+        if len(shape) != 2 or shape[1] != F:
+            raise ValueError(f"{what}: expected a matrix of {F} features a workload")
+        rows = shape[0]
+        return self._flat(x, torch.float32, rows * F, what), rows
 
     def predictor_loss_work(self, pred, count):
         """Bytes of scratch predictor_loss needs."""
@@ -288,30 +290,28 @@ class Context:
         dictionary of tensors shaped like the predictor's parameters, its gradients.  on, off: int32, out of range
         (-1) for samples that only fill the batch; target: float32, NaN where not measured.  dropout: (p, seed) or
         (p, seed, step).  scale: 1 / number of samples if not given."""
-        count = on.numel() if isinstance(on, torch.Tensor) else 0
-        flat = lambda t, what: self._flat(t, torch.float32, count, what, optional=True)
-        sides = self._sides(pred, x_on, x_off)
-        samples = Samples(self._flat(on, torch.int32, count, "on"), self._flat(off, torch.int32, count, "off"),
-                          self._flat(target, torch.float32, count, "target"), flat(target_slow, "target_slow"), count)
-        rule = self._dropout(*dropout, *((0,) if len(dropout) == 2 else ())) if dropout is not None else None
+        count, F, H, flat, f32, i32 = on.numel() if isinstance(on, torch.Tensor) else 0, pred.F, pred.H, self._flat, torch.float32, torch.int32
+        p_on, n = self._side(x_on, F, "x_on")
+        p_off, m = self._side(x_off, F, "x_off")
+        samples = SAMPLES.pack(flat(on, i32, count, "on"), flat(off, i32, count, "off"), flat(target, f32, count, "target"),
+                               0 if target_slow is None else flat(target_slow, f32, count, "target_slow"), count)
         if grads is not None:
-            F, H = pred.F, pred.H
-            grads = Gradients(*[self._flat(grads[name], torch.float32, size(F, H), name) if getattr(pred, member) is not None else None
-                                for member, name, size in PARAMETERS])
+            grads = GRADIENTS.pack(*[0 if getattr(pred, member) is None else flat(grads[name], f32, columns * F + units * H + ones + squares * H * H + both * F * H, name)
+                                     for member, name, (columns, units, ones, squares, both) in PARAMETERS])
         work = self._work(work, self.predictor_loss_work, pred, count)
         self._check(_lib.mf_predictor_loss(
-            self._h, C.byref(pred), *sides, C.byref(samples), C.byref(rule) if rule is not None else None,
-            1.0 / max(count, 1) if scale is None else float(scale), C.byref(grads) if grads is not None else None,
-            self._flat(loss, torch.float32, 1, "loss"), flat(sigma, "sigma"), flat(sigma_slow, "sigma_slow"),
-            work.data_ptr(), work.numel()))
+            self._h, C.byref(pred), p_on, n, p_off, m, samples, None if dropout is None else self._dropout(*dropout),
+            1.0 / max(count, 1) if scale is None else float(scale), grads, flat(loss, f32, 1, "loss"), None if sigma is None else flat(sigma, f32, count, "sigma"),
+            None if sigma_slow is None else flat(sigma_slow, f32, count, "sigma_slow"), work.data_ptr(), work.numel()))
 
     def predict_pairs(self, pred, x_on, x_off, on, off, sigma, sigma_slow=None):
         """sigma[s] (and sigma_slow[s]) = what the predictor says of the pair (on[s], off[s])."""
-        count = on.numel() if isinstance(on, torch.Tensor) else 0
+        count, F = on.numel() if isinstance(on, torch.Tensor) else 0, pred.F
+        p_on, n = self._side(x_on, F, "x_on")
+        p_off, m = self._side(x_off, F, "x_off")
         self._check(_lib.mf_predict_pairs(
-            self._h, C.byref(pred), *self._sides(pred, x_on, x_off), self._flat(on, torch.int32, count, "on"),
-            self._flat(off, torch.int32, count, "off"), count, self._flat(sigma, torch.float32, count, "sigma"),
-            self._flat(sigma_slow, torch.float32, count, "sigma_slow", optional=True)))
+            self._h, C.byref(pred), p_on, n, p_off, m, self._flat(on, torch.int32, count, "on"), self._flat(off, torch.int32, count, "off"), count,
+            self._flat(sigma, torch.float32, count, "sigma"), None if sigma_slow is None else self._flat(sigma_slow, torch.float32, count, "sigma_slow")))
 
     def predictor(self, params, scale, mem_feature=0, mem_limit=1.0, sm=None, slow_limit=None, norm_eps=None):
         """params: dict of float32 device tensors W1 [H,2F], b1, W2 [H,H], b2, W3 [H], b3 [1];
