@@ -453,6 +453,83 @@ def test_an_update_scores_again_with_the_norm(ctx):
     assert torch.equal(W[:, :m], fresh[:, :m])
 
 
+def shifted(t):
+    """The same values, beginning four bytes beyond a multiple of sixteen."""
+    buf = torch.empty(t.numel() + 8, dtype=t.dtype, device="cuda")
+    out = buf[1:1 + t.numel()].view(t.shape)
+    assert out.data_ptr() % 16 == 4
+    return out.copy_(t)
+
+
+@pytest.mark.parametrize("H, F, norm, count", [(64, 16, True, 300), (128, 32, True, 300), (64, 50, False, 300), (128, 70, True, 300), (64, 16, True, 5000), (128, 17, False, 5000)])
+def test_tensors_that_begin_anywhere(ctx, H, F, norm, count):
+    """Features, samples, weights but those of the hidden layer and the output unit, and gradients, aligned to nothing but their values."""
+    s = problem(50, count, F, H, norm=norm, slow=True)
+    params = {k: v if k in ("W2", "b2", "W3", "W3slow") else shifted(v) for k, v in dev_params(s["params"]).items()}
+    pred = ctx.predictor(params, 1.0, slow_limit=0.5, norm_eps=s["eps"])
+    x_on, x_off, on, off, target, slow = (shifted(dev(s[k])) for k in ("x_on", "x_off", "on", "off", "target", "target_slow"))
+    out = {"loss": shifted(torch.zeros(1, device="cuda")), "sigma": shifted(torch.zeros(count, device="cuda")), "sigma_slow": shifted(torch.zeros(count, device="cuda"))}
+    grads = {k: shifted(torch.zeros(v.shape, device="cuda")) for k, v in s["params"].items()}
+    ctx.predictor_loss(pred, x_on, x_off, on, off, target, out["loss"], grads=grads, target_slow=slow, sigma=out["sigma"], sigma_slow=out["sigma_slow"])
+    compare({k: v.cpu().numpy() for k, v in {**out, **grads}.items()}, definition(s))
+    sigma = shifted(torch.zeros(count, device="cuda"))
+    ctx.predict_pairs(pred, x_on, x_off, on, off, sigma)
+    ref.within(sigma.cpu().numpy(), *definition(s)["sigma"], "sigma")
+
+
+def test_two_graphs_of_a_context_replayed_in_turn(ctx):
+    """Both use the context's scratch: one predictor has many features, the other no norm; with eager calls of the context between them."""
+    import paper_2303_13803_amd as mm
+    stream = torch.cuda.Stream()
+    mine = mm.Context(1, 1, stream=stream)
+    problems = [problem(60, 700, 100, 64, missing=True), problem(61, 900, 20, 64, norm=False, sm=True), problem(62, 800, 30, 64, sm=True)]
+    calls, expected, graphs = [], [call(ctx, s, (0.1, 2, 3)) for s in problems], []
+    for s in problems:
+        pred, t = predictor(mine, s), {k: dev(s[k]) for k in ("x_on", "x_off", "on", "off", "target")}
+        out = {"loss": torch.zeros(1, device="cuda"), "grads": {k: torch.zeros(v.shape, device="cuda") for k, v in s["params"].items()},
+               "sigma": torch.zeros(len(s["on"]), device="cuda"), "work": torch.empty(mine.predictor_loss_work(pred, len(s["on"])), dtype=torch.uint8, device="cuda")}
+        calls.append((pred, t, out))
+    torch.cuda.synchronize()
+    for pred, t, out in calls[:2]:
+        graphs.append(torch.cuda.CUDAGraph())
+        with torch.cuda.graph(graphs[-1], stream=stream):
+            mine.predictor_loss(pred, **t, **out, dropout=(0.1, 2, 3))
+    for _ in range(3):
+        for pred, t, out in calls:
+            out["loss"].zero_()
+            out["sigma"].zero_()
+            for g in out["grads"].values():
+                g.zero_()
+        torch.cuda.synchronize()
+        with torch.cuda.stream(stream):
+            graphs[0].replay()
+            mine.predictor_loss(calls[2][0], **calls[2][1], **calls[2][2], dropout=(0.1, 2, 3))
+            graphs[1].replay()
+        torch.cuda.synchronize()
+        for (_, _, out), e in zip(calls, expected):
+            assert (out["loss"].cpu().numpy() == e["loss"]).all() and (out["sigma"].cpu().numpy() == e["sigma"]).all()
+            for k, g in out["grads"].items():
+                assert (g.cpu().numpy() == e[k]).all(), k
+    mine.close()
+
+
+def test_scratch_of_the_librarys_own_in_the_order_of_its_stream(ctx):
+    """A context on a stream that is not the current one, and no scratch given: what the allocator hands out next on the current stream is another's."""
+    import paper_2303_13803_amd as mm
+    mine = mm.Context(1, 1, stream=torch.cuda.Stream())
+    s = problem(63, 20000, 32, 128, n=300, m=300)
+    expected = call(ctx, s, (0.1, 2, 3))
+    t, pred = {k: dev(s[k]) for k in ("x_on", "x_off", "on", "off", "target")}, predictor(mine, s)
+    loss, grads = torch.zeros(1, device="cuda"), {k: torch.zeros(v.shape, device="cuda") for k, v in s["params"].items()}
+    torch.cuda.synchronize()
+    for _ in range(3):
+        mine.predictor_loss(pred, **t, loss=loss, grads=grads, dropout=(0.1, 2, 3))
+        torch.full((mine.predictor_loss_work(pred, 20000),), 255, dtype=torch.uint8, device="cuda")
+    torch.cuda.synchronize()
+    assert (loss.cpu().numpy() == expected["loss"]).all() and all((g.cpu().numpy() == expected[k]).all() for k, g in grads.items())
+    mine.close()
+
+
 def test_two_contexts_at_once(ctx):
     """Two fits on two streams, each with its own scratch."""
     import paper_2303_13803_amd as mm
