@@ -29,7 +29,7 @@
 //
 // Measured: a million samples of 32 features a workload through 128 units, with every option, 0.51 ms, 263 TFLOP/s where float32's matrix
 // instructions reach 152; the matrix pipe is busy a third of that, and either kind of wavefront takes some 2000 cycles for each of the four
-// stages, its own chain of LDS reads, products and arithmetic.  2000 samples of 16 features through 64 units 20 us; 200,003 predictions 62.
+// stages, its own chain of LDS reads, products and arithmetic.  2000 samples of 16 features through 64 units 19 us; 200,003 predictions 61.
 //
 // NaN: a ReLU that is one instruction turns it into 0, so what is not finite among the weights, or a sample's features, is added to the output as a NaN.
 #include "fit_parts.h"
@@ -925,7 +925,7 @@ int run_fit(mf_ctx *ctx, const mf_predictor *p, const float *d_on, int n, const 
     FitArgs a{};
     a.X[0] = n > 0 ? d_on : ctx->fit_W1; a.X[1] = m > 0 ? d_off : ctx->fit_W1;      // (a row that can be read where there is none)
     a.rows[0] = n; a.rows[1] = m;
-    a.F = p->F; a.columns = f.columns; a.padded = f.padded; a.half = f.half;
+    a.F = p->F; a.padded = f.padded; a.half = f.half;
     a.index[0] = s->d_on; a.index[1] = s->d_off;
     a.target[0] = s->d_target; a.target[1] = s->d_target_slow;
     a.sigma[0] = d_sigma; a.sigma[1] = d_sigma_slow;

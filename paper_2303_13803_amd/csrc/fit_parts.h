@@ -17,7 +17,7 @@ constexpr int FIT_RANGE_PARTS = 256;                        // workgroups that l
 
 struct FitArgs {
     const float *X[2];
-    int rows[2], F, columns, padded, half;                  // columns = 2F; laid out as [0, F) and [half, half + F) of `padded` ones
+    int rows[2], F, padded, half;                           // the 2F columns of layer 1 are laid out as [0, F) and [half, half + F) of `padded` ones
     const int32_t *index[2];
     const float *target[2];                                 // throughput, slowdown (null: not trained)
     float *sigma[2];                                        // (null: not wanted)

@@ -361,7 +361,6 @@ void mf_plan_wide(const mf_ctx *ctx, long long count, FitPlan *f)
 {
     f->half = f->columns / 2;
     f->padded = (f->columns + 31) & ~31;
-    f->tiles = FIT_WIDE_TILES;
     const int chunks = (f->padded + FIT_CHUNK - 1) / FIT_CHUNK;
     f->passes = (chunks + FIT_WIDE_TILES - 1) / FIT_WIDE_TILES;
     const long long tiles = (count + FIT_ROWS - 1) / FIT_ROWS, units = (ctx->n_cus > 0 ? ctx->n_cus : 256) * (f->H == 64 ? 2 : 1);

@@ -10,8 +10,8 @@
 // stored unaligned, and the one that would reach over a row's end is moved back to end with it; what it
 // then holds twice is written twice, the same bits, and counted once.
 //
-// Measured (read and written bytes over time; a large copy reaches 4.7 TB/s): the norm of 1,000,003 x 128 bfloat16 5.3 TB/s, its gradient of 131,072 x 1024 float16
-// 5.1, dropout of 500,009 x 251 bfloat16 6.0.  Of 2000 x 64 float32 values the gradient takes 4 us and its sums 2, dropout 2; the norm of 64 x 16 1.7.
+// Measured (read and written bytes over time; a large copy reaches 4.7 TB/s): the norm of 1,000,003 x 128 bfloat16 5.2 TB/s, its gradient of 131,072 x 1024 float16
+// 5.0, dropout of 500,009 x 251 bfloat16 6.0.  Of 2000 x 64 float32 values the gradient takes 4 us and its sums 2, dropout 2; the norm of 64 x 16 1.7.
 #include "internal.h"
 #include "philox.h"
 #include "row_sums.h"
