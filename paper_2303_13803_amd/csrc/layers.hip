@@ -357,6 +357,8 @@ bool good_rows(const void *p, int type, int64_t rows, int64_t width, int64_t ld)
 {
     return p && whole_values(p, type) && ld >= width && (rows < 2 || ld <= (1ll << 50) / rows);
 }
+// What is written in the place of what is read has to have its pitch.
+bool same_place(const void *from, int64_t ld, const void *to, int64_t ldo, int64_t rows) { return from != to || ld == ldo || rows < 2; }
 
 }  // namespace
 
@@ -379,7 +381,7 @@ int mf_layer_norm(mf_ctx *ctx, int type, const void *d_x, int64_t rows, int64_t 
     if (rc != MF_OK) return rc;
     if (!d_w || !d_b || !(eps > 0.0f) || isinf(eps) || !whole_values(d_w, MF_F32) || !whole_values(d_b, MF_F32)) return MF_ERR_ARG;
     if (rows == 0) return MF_OK;
-    if (!good_rows(d_x, type, rows, width, ldx) || !good_rows(d_y, type, rows, width, ldy)) return MF_ERR_ARG;
+    if (!good_rows(d_x, type, rows, width, ldx) || !good_rows(d_y, type, rows, width, ldy) || !same_place(d_x, ldx, d_y, ldy, rows)) return MF_ERR_ARG;
     MF_HIP(hipSetDevice(ctx->device));
     NormArgs a{};
     a.x = d_x; a.out = d_y;
@@ -406,6 +408,7 @@ int mf_layer_norm_grad(mf_ctx *ctx, int type, const void *d_x, int64_t rows, int
     if (!whole_values(d_w, MF_F32) || !whole_values(d_dw, MF_F32) || !whole_values(d_db, MF_F32)) return MF_ERR_ARG;
     if (rows > 0) {
         if (!good_rows(d_x, type, rows, width, ldx) || !good_rows(d_dy, type, rows, width, lddy) || !good_rows(d_dx, type, rows, width, lddx)) return MF_ERR_ARG;
+        if (!same_place(d_x, ldx, d_dx, lddx, rows) || !same_place(d_dy, lddy, d_dx, lddx, rows)) return MF_ERR_ARG;
         if (!d_work || ((uintptr_t)d_work & 15u) || work_bytes < mf_layer_norm_grad_work(ctx, rows, width)) return MF_ERR_ARG;
     }
     MF_HIP(hipSetDevice(ctx->device));
@@ -429,7 +432,7 @@ int mf_dropout(mf_ctx *ctx, int type, const void *d_x, int64_t rows, int64_t wid
     DropArgs a{};
     if (!rule || !mf_drop_rule(rule, &a.rule) || layer < 0 || layer > 65535) return MF_ERR_ARG;
     if (rows == 0) return MF_OK;
-    if (!good_rows(d_x, type, rows, width, ldx) || !good_rows(d_y, type, rows, width, ldy)) return MF_ERR_ARG;
+    if (!good_rows(d_x, type, rows, width, ldx) || !good_rows(d_y, type, rows, width, ldy) || !same_place(d_x, ldx, d_y, ldy, rows)) return MF_ERR_ARG;
     MF_HIP(hipSetDevice(ctx->device));
     a.x = d_x; a.y = d_y;
     a.total = rows * width; a.ldx = ldx; a.ldy = ldy; a.width = (int)width;

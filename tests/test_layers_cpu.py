@@ -145,6 +145,14 @@ def test_dropout_refuses(lib, ctx, change, rule):
     assert lib.raw_library().mf_dropout(ctx, *{**a, **change}.values()) == lib.ERR_ARG
 
 
+def test_layers_refuse_to_write_in_place_with_another_pitch(lib, ctx):
+    raw, rule = lib.raw_library(), lib.DropoutRule(0.5, 1, 2, None)
+    assert raw.mf_layer_norm(ctx, *_norm(ldy=9)) == lib.ERR_ARG
+    assert raw.mf_dropout(ctx, 0, A, 3, 8, 9, C.byref(rule), 0, A, 8) == lib.ERR_ARG
+    for x, ldx, dy, lddy, dx, lddx in ((A, 8, 2 * A, 8, A, 9), (A, 8, 2 * A, 9, 2 * A, 8)):
+        assert raw.mf_layer_norm_grad(ctx, 0, x, 3, 8, ldx, dy, lddy, A, 1e-5, dx, lddx, A, A, A, 1 << 20) == lib.ERR_ARG
+
+
 def _predictor(lib, **change):
     p = dict(F=16, H=64, scale=1.0, mem_feature=0, mem_limit=1.0, d_W1=A, d_b1=A, d_W2=A, d_b2=A, d_W3=A, d_b3=A, d_W1sm=None, sm_on_feature=0, sm_off_feature=0,
              d_W3_slow=None, d_b3_slow=None, slow_limit=0.0, d_ln_w=A, d_ln_b=A, ln_eps=1e-5)
