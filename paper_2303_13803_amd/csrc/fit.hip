@@ -374,14 +374,26 @@ __global__ __launch_bounds__(H * 4, 2) void fit_kernel(const FitArgs a, const fl
             const float share = fabsf(fminf(1.0f - on, off));
             if (share < INFINITY) v[1] = fmaxf(v[1], share);
         }
-    if (GRAD)                                               // this workgroup's own targets
-#pragma unroll 4
-        for (int it = tid / T; it < mine; it += H * 4 / T) {
-            const long long s = tile_of(it) * T + tid % T, at = s < a.count ? s : a.count - 1;
+    if (GRAD) {                                             // this workgroup's own targets, and 1, which shares of a throughput stay below
+        const auto most_at = [&](const int it, long long &at) {
+            const long long s = tile_of(it) * T + tid % T;
+            at = s < a.count ? s : a.count - 1;
             const float t = fabsf(a.target[0][at]), ts = slow ? fabsf(a.target[1][at]) : 0.0f;
-            if (t < INFINITY) v[0] = fmaxf(v[0], t);
-            if (ts < INFINITY) v[0] = fmaxf(v[0], ts);
+            return fmaxf(t < INFINITY ? t : 0.0f, ts < INFINITY ? ts : 0.0f);
+        };
+        long long at;
+        v[0] = 1.0f;
+#pragma unroll 4
+        for (int it = tid / T; it < mine; it += H * 4 / T) v[0] = fmaxf(v[0], most_at(it, at));
+        if (v[0] > 1.0f) {                                  // only of samples that name a pair: others may have anything there
+            v[0] = 1.0f;
+#pragma unroll 1
+            for (int it = tid / T; it < mine; it += H * 4 / T) {
+                const float most = most_at(it, at);
+                if ((unsigned)a.index[0][at] < (unsigned)a.rows[0] && (unsigned)a.index[1][at] < (unsigned)a.rows[1]) v[0] = fmaxf(v[0], most);
+            }
         }
+    }
 #pragma unroll
     for (int q = 0; q < 9; ++q) {
         v[q] = wave_max(v[q]);
