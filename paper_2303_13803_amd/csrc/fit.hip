@@ -902,10 +902,10 @@ int launch_fit(mf_ctx *ctx, const FitArgs &a, const FitPlan &f)
 {
     const int bytes = (int)sizeof(FitShared<H, CT, GRAD>);
     static_assert(sizeof(FitShared<H, CT, GRAD>) <= 160 * 1024, "LDS");
-    const unsigned flag = 1u << ((H == 128 ? 16 : 0) + (GRAD ? 8 : 0) + (EXTRA ? 4 : 0) + CT - 1);
-    if (!(ctx->fit_configured & flag)) {
+    constexpr unsigned long long flag = lds_bit_fit(H, CT, GRAD, EXTRA);
+    if (!(ctx->kernels_configured & flag)) {
         MF_HIP(hipFuncSetAttribute((const void *)fit_kernel<H, CT, GRAD, EXTRA>, hipFuncAttributeMaxDynamicSharedMemorySize, bytes));
-        ctx->fit_configured |= flag;
+        ctx->kernels_configured |= flag;
     }
     hipLaunchKernelGGL((fit_kernel<H, CT, GRAD, EXTRA>), dim3(f.grid), dim3(H * 4), bytes, ctx->stream, a, ctx->fit_W1 + FOLD_RANGES, f.parts);
     MF_HIP(hipGetLastError());

@@ -343,7 +343,7 @@ __global__ __launch_bounds__(H * 4) void wide_kernel(const FitArgs a, const floa
 template <int H, int GT, bool GRAD>
 int launch_wide(mf_ctx *ctx, const FitArgs &a, const FitPlan &f, const float *ranges)
 {
-    const unsigned flag = 1u << (21 + (H == 128 ? 2 : 0) + (GRAD ? 1 : 0));
+    constexpr unsigned long long flag = lds_bit_wide(H, GRAD);
     if (!(ctx->kernels_configured & flag)) {
         MF_HIP(hipFuncSetAttribute((const void *)wide_kernel<H, GT, GRAD>, hipFuncAttributeMaxDynamicSharedMemorySize, (int)wide_lds_bytes<H>(GRAD)));
         ctx->kernels_configured |= flag;

@@ -4,6 +4,7 @@
 #include <stdint.h>
 #include <tuple>
 #include "muxmatch.h"
+#include "lds_bits.h"
 #include "pair_tasks.h"
 #include "side_end.h"
 
@@ -173,7 +174,7 @@ struct mf_ctx : mf_options {
     hipStream_t stream;
     int max_n, max_m;
     hipError_t hip_error;
-    unsigned kernels_configured;    // kernels whose dynamic shared memory limit has been raised on this device (bits)
+    unsigned long long kernels_configured;      // kernels whose dynamic shared memory limit has been raised on this device (lds_bits.h)
     // scoring scratch
     float *proj_on, *proj_off;      // [max_n][H], [max_m][H]
     float *mem_on, *mem_off;        // [max_n], [max_m]
@@ -236,7 +237,6 @@ struct mf_ctx : mf_options {
     unsigned *score_range;              // device: largest magnitudes the scorer's fp16 pieces are scaled by (project_kernel)
     mf_cert_out *h_cert;
     float *fit_W1;                      // device, MF_FIT_SCRATCH floats: layer 1 with the norm folded in, and what bounds a fit's values (fit.hip)
-    unsigned fit_configured;            // as kernels_configured, of the kernels of fit.hip
     // timing
     unsigned long long *times, *h_times;        // [AT_COUNT] device, pinned
     double clock_khz;               // of the clock they are in

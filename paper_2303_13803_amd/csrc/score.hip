@@ -957,7 +957,7 @@ int launch_pair_variant(mf_ctx *ctx, const mf_predictor *p, int n, int m, int32_
 {
     using S = PairShape<H>;
     // (the attribute belongs to the device, so what has been set is remembered per context)
-    const unsigned flag = 1u << (5 + (H == 128 ? 8 : 0) + (PAIR_SM ? 4 : 0) + (SLOWDOWN ? 2 : 0) + (SPLIT ? 1 : 0));
+    constexpr unsigned long long flag = lds_bit_pair(H, PAIR_SM, SLOWDOWN, SPLIT);
     if (!(ctx->kernels_configured & flag)) {
         for (const auto kernel : {pair_mlp_kernel<H, PAIR_SM, SLOWDOWN, SPLIT, false>, pair_mlp_kernel<H, PAIR_SM, SLOWDOWN, SPLIT, true>})
             MF_HIP(hipFuncSetAttribute((const void *)kernel, hipFuncAttributeMaxDynamicSharedMemorySize, (int)S::LDS_BYTES));

@@ -298,7 +298,7 @@ template <int C>
 int launch_small(mf_ctx *ctx, const SmallShape &s, const int32_t *d_W, long long K, int32_t *d_row2col, int64_t *d_u, int64_t *d_v)
 {
     static_assert(SMALL_COLS == 64 * 8, "the widest instance");
-    const unsigned flag = 1u << (C == 1 ? 21 : (C == 2 ? 22 : (C == 4 ? 23 : 24)));
+    constexpr unsigned long long flag = lds_bit_small(C);
     if (!(ctx->kernels_configured & flag)) {
         MF_HIP(hipFuncSetAttribute((const void *)small_kernel<C>, hipFuncAttributeMaxDynamicSharedMemorySize, SMALL_LDS));
         ctx->kernels_configured |= flag;
