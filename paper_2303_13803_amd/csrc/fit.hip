@@ -46,15 +46,16 @@ namespace {
 
 constexpr int FIT_ROWS = 32;
 
-// The largest power of two that takes a value of at most `bound` to below 2^14 (1 for bounds that are none).
-__device__ __forceinline__ float scale_below(float bound)
+// The exponent of the largest power of two that takes a value of at most `bound` to below 2^14 (0 for bounds that are none).
+__device__ __forceinline__ int exponent_below(float bound)
 {
-    if (!(bound > 0.0f) || bound > 1e30f) return 1.0f;
+    if (!(bound > 0.0f) || bound > 1e30f) return 0;
     int e;
     (void)frexpf(bound, &e);                                // bound < 2^e
     e = e < -96 ? -96 : e > 96 ? 96 : e;
-    return ldexpf(1.0f, 14 - e);
+    return 14 - e;
 }
+__device__ __forceinline__ float scale_below(float bound) { return ldexpf(1.0f, exponent_below(bound)); }
 
 // v = hi + lo in fp16, to 22 bits.  The remainder is exact; written as a fused multiply-add by a -1 that the optimiser cannot see it is one
 // instruction that reads the fp16 piece itself.
@@ -292,7 +293,7 @@ __global__ __launch_bounds__(H * 4, 2) void fit_kernel(const FitArgs a, const fl
     // ---- bounds, and the scales that follow.  Weights are read as the operands that the forward wavefronts make of them: layer 1's with the
     // norm's weight, W2's transpose (or, without a way back, W2), a unit's in two lanes.
     float w[KB][8], u1[XB][8], bias1 = 0.0f, poison = 0.0f;
-    // largest of: targets, features (or, of those that a norm bounds, SM shares), output weights of either unit, weights of layers 2 and 1, columns' sums of W2, z1 without features and for each
+    // largest of: targets, features (or, of those that a norm bounds, the SM share's two), output weights of either unit, weights of layers 2 and 1, columns' sums of W2, z1 without features and for each
     float v[9] = {0.0f, 0.0f, 0.0f, 0.0f, 0.0f, 0.0f, 0.0f, 0.0f, 0.0f};
     const float length = sqrtf((float)a.F);
     const auto read_w2 = [&](const int b, float (&to)[8]) {
@@ -365,15 +366,6 @@ __global__ __launch_bounds__(H * 4, 2) void fit_kernel(const FitArgs a, const fl
         poison += a.b2[tid] * 0.0f;
     }
     if (tid < parts) v[1] = ranges[tid];
-    if (!GRAD && EXTRA && with_share && parts == 0)         // nothing else bounds the share: this workgroup's own
-#pragma unroll 4
-        for (int it = tid / T; it < mine; it += H * 4 / T) {
-            const long long s = tile_of(it) * T + tid % T, at = s < a.count ? s : a.count - 1;
-            const int i = a.index[0][at], j = a.index[1][at];
-            const float on = a.X[0][((unsigned)i < (unsigned)a.rows[0] ? i : 0) * a.F + a.sm_feature[0]], off = a.X[1][((unsigned)j < (unsigned)a.rows[1] ? j : 0) * a.F + a.sm_feature[1]];
-            const float share = fabsf(fminf(1.0f - on, off));
-            if (share < INFINITY) v[1] = fmaxf(v[1], share);
-        }
     if (GRAD) {                                             // this workgroup's own targets, and 1, which shares of a throughput stay below
         const auto most_at = [&](const int it, long long &at) {
             const long long s = tile_of(it) * T + tid % T;
@@ -422,7 +414,11 @@ __global__ __launch_bounds__(H * 4, 2) void fit_kernel(const FitArgs a, const fl
     const float s_x = scale_below(a.norm ? length * 1.001f : v[1]), s_w2 = scale_below(v[4]), s_w1 = scale_below(v[5]);
     const float bound2 = 0.5f * (1.0f + v[0]) * (v[2] + v[3]) * factor * 1.001f;
     const float s_dz2 = scale_below(bound2), s_dz1 = scale_below(bound2 * factor * v[6] * 1.001f);
-    const float s_d1 = scale_below((v[7] + v[8] * v[1]) * factor * 1.001f);
+    // Without gradients a lane of the forward wavefronts has a sample of its own, whose SM share, where nothing bounds it, scales what is its own and
+    // nobody else's (OWN: then by_z1, by_z2, sh.b1 and sh.wsm lack that scale).
+    constexpr bool OWN = !GRAD && EXTRA;
+    const float s_d1 = OWN ? 1.0f : scale_below((v[7] + v[8] * v[1]) * factor * 1.001f);
+    const float most_d1 = (v[7] + (a.norm ? 0.0f : v[8] * v[1])) * factor * 1.001f, most_share = a.norm ? v[8] * factor * 1.001f : 0.0f;
     // what accumulators of the three products are multiplied with
     const float by_z1 = factor * s_d1 / (s_x * s_w1), by_z2 = factor / (s_d1 * s_w2), by_d1 = factor * s_dz1 / (s_dz2 * s_w2), by_dz = factor * s_dz2;
     if (tid < H) {
@@ -499,7 +495,10 @@ __global__ __launch_bounds__(H * 4, 2) void fit_kernel(const FitArgs a, const fl
 #pragma unroll
                 for (int b = 0; b < XB; ++b) z = product(w1[b], x[b], b == 0 ? zero : z);
             }
-            const float share = with_share ? sh.share[it & 3][nn] : 0.0f;
+            float share = with_share ? sh.share[it & 3][nn] : 0.0f;
+            const int own_scale = OWN ? exponent_below(fmaf(most_share, fabsf(share), most_d1)) : 0;
+            const float s_own = ldexpf(1.0f, own_scale), by_z1_here = OWN ? by_z1 * s_own : by_z1, by_z2_here = OWN ? ldexpf(by_z2, -own_scale) : by_z2;
+            if (OWN) share *= s_own;
 #pragma unroll
             for (int g = 0; g < 2; ++g) {
                 const unsigned keep = a.drop ? sh.keep[now][0][nn][4 * ub + hh + 2 * g] : 255u;
@@ -507,7 +506,7 @@ __global__ __launch_bounds__(H * 4, 2) void fit_kernel(const FitArgs a, const fl
 #pragma unroll
                 for (int e = 0; e < 8; ++e) {
                     const int k = u0 + 16 * g + e;
-                    float h = fmaf(z[8 * g + e], by_z1, sh.b1[k]);
+                    float h = fmaf(z[8 * g + e], by_z1_here, OWN ? sh.b1[k] * s_own : sh.b1[k]);
                     if (EXTRA) h = fmaf(share, sh.wsm[k], h);
                     v[e] = kept(h, keep, e);
                     open1[8 * g + e] = v[e] > 0.0f;
@@ -528,7 +527,7 @@ __global__ __launch_bounds__(H * 4, 2) void fit_kernel(const FitArgs a, const fl
 #pragma unroll
                 for (int e = 0; e < 8; ++e) {
                     const int k = u0 + 16 * g + e;
-                    const float h = kept(fmaf(z[8 * g + e], by_z2, sh.b2[k]), keep, e);
+                    const float h = kept(fmaf(z[8 * g + e], by_z2_here, sh.b2[k]), keep, e);
                     h2[8 * g + e] = h;
                     zp = fmaf(sh.w3[0][k], h, zp);
                     if (EXTRA) zs = fmaf(sh.w3[1][k], h, zs);
@@ -959,10 +958,8 @@ int run_fit(mf_ctx *ctx, const mf_predictor *p, const float *d_on, int n, const 
     a.partial_step = f.step(g != nullptr);
     float *const ranges = ctx->fit_W1 + FOLD_RANGES;
     FitArgs folded = a;                                     // as wide_kernel takes it
-    // A workgroup of predictions looks up the SM shares of up to 2048 samples by itself; for more the launch before is no dearer (without and with it, 32 features
-    // and 128 units: 2000 pairs 13 and 18 us, 300,000 91 and 96, a million 261 and 260, three 760 and 736).  With gradients the launch stays: the code for
-    // it, never run, made the loss of a million samples 505 -> 539 us, by what the compiler then keeps in registers of the loop over samples.
-    const bool share_first = a.norm && a.W1sm && (g || a.count > 2048ll * f.grid), fallback = !f.wide && !a.norm, look = !f.wide && (!a.norm || share_first);
+    // (predictions scale by every sample's own SM share)
+    const bool share_first = a.norm && a.W1sm && g, fallback = !f.wide && !a.norm, look = !f.wide && (!a.norm || share_first);
     if (f.wide || look) {
         FoldArgs w{};
         w.W1 = p->d_W1; w.b1 = p->d_b1; w.g = p->d_ln_w; w.beta = p->d_ln_b;

@@ -1,9 +1,12 @@
 """GPU: samples and workloads that stand out do not change what is said of the others."""
 import numpy as np
 import pytest
+import torch
 
 import fit_close as close
-from test_gpu_fit import call, problem
+import fit_reference as ref
+from gpu_util import dev
+from test_gpu_fit import SM, call, definition, predictor, problem
 
 pytestmark = pytest.mark.gpu
 
@@ -19,6 +22,12 @@ def ctx():
 def same_bits(a, b, names):
     for name in names:
         assert (a[name].view(np.int32) == b[name].view(np.int32)).all(), name
+
+
+def predictions(ctx, s):
+    out = [torch.full((len(s["on"]),), 7.0, device="cuda") for _ in range(2 if s["target_slow"] is not None else 1)]
+    ctx.predict_pairs(predictor(ctx, s), dev(s["x_on"]), dev(s["x_off"]), dev(s["on"]), dev(s["off"]), *out)
+    return dict(zip(("sigma", "sigma_slow"), (o.cpu().numpy() for o in out)))
 
 
 # ---- targets of samples that name no pair
@@ -39,3 +48,34 @@ def test_targets_of_samples_that_name_no_pair(ctx, fill, count, F, H):
     same_bits(plain, filled, plain)
     s = close.away_from_kinks(s, (0.1, 2, 3))
     close.check(call(ctx, s, (0.1, 2, 3)), close.room(s, (0.1, 2, 3), longest=count / 64))
+
+
+# ---- an SM feature that is no fraction.  Workload 7 and workload 9 have it, so that only a pair of both has a share of that size:
+# min(1 + v, v); beside others either's share is an ordinary one.
+
+def with_large_shares(seed, count, H, value, F=16, **kw):
+    s = problem(seed, count, F, H, norm=True, sm=True, slow=True, **kw)
+    s["x_on"][7, SM[0]], s["x_off"][9, SM[1]] = -value, value
+    both = (s["on"] == 7) & (s["off"] == 9)
+    s["on"][both] = 8
+    return s
+
+
+@pytest.mark.parametrize("H", [64, 128])
+@pytest.mark.parametrize("count", [1000, 5003, 20001])
+@pytest.mark.parametrize("value", [5e3, 1e9, 1e12, 1e18])
+@pytest.mark.parametrize("named", [False, True])
+def test_predictions_beside_a_large_sm_share(ctx, named, value, count, H):
+    """As few pairs are predicted and as many are; 1e-5 of every prediction, and of the pair with that share what its own sums may be off.  (Squares of
+    features beyond 1.8e19 pass the largest float32, 3.4e38, and with them that row's variance.)"""
+    s = with_large_shares(71, count, H, value)
+    if named:
+        s["on"][17], s["off"][17] = 7, 9
+    with np.errstate(over="ignore"):
+        expected = definition(s)
+    got = predictions(ctx, s)
+    others = np.arange(count) != (17 if named else -1)
+    for name in got:
+        value64, bound = expected[name]
+        assert (np.abs(got[name] - value64)[others] <= 1e-5 * value64[others]).all(), name
+        ref.within(got[name][~others], value64[~others], bound[~others], name)
