@@ -16,8 +16,8 @@
 // from a bound on it that is never exceeded, to below 2^14; what is within 2^-17 of the bound keeps all its 22 bits, smaller
 // values lose absolute precision of 2^-39 of the bound.  The bounds: a normalised row has |u|_2 <= sqrt(F), so |z1_k| <= |W1_k|_2
 // sqrt(2F) + |b1_k|; |dz3| <= (1 + max |t|) / 2; and through W3 and W2 by their largest values and columns' sums.  Features that no norm
-// bounds are looked for; where one is above FIT_LARGEST all of it is done once more in float32 products (wide_kernel), so that what others keep does not
-// depend on it.
+// bounds, those of an SM share behind a norm among them, are looked for; where one is above FIT_LARGEST all of it is done once more in float32 products
+// (wide_kernel), so that what others keep does not depend on it.  Without gradients a sample is scaled by its own SM share instead.
 //
 // A workgroup takes FIT_ROWS samples at a time.  Half of its wavefronts ("forward", 32 hidden units each) take them through the layers and back;
 // activations pass between them through LDS.  The others ("sums") add up the gradients of weights, in accumulators that stay until there are no
@@ -182,10 +182,15 @@ __global__ __launch_bounds__(256) void fold_kernel(FoldArgs a)
             const int32_t *index = k ? a.index[1] : a.index[0];
             const int rows = k ? a.rows[1] : a.rows[0];
             const long long all = (a.listed ? a.count : rows) * a.width;
+            const int32_t *other = k ? a.index[0] : a.index[1];
+            const int other_rows = k ? a.rows[0] : a.rows[1];
 #pragma unroll 8
             for (long long e = first; e < all; e += step) {
                 int row = (int)(e / a.width);
-                if (a.listed) row = index[row];
+                if (a.listed) {                             // (of samples that name a pair)
+                    if ((unsigned)other[row] >= (unsigned)other_rows) continue;
+                    row = index[row];
+                }
                 if ((unsigned)row >= (unsigned)rows) continue;
                 const float v = fabsf(X[(size_t)row * a.F + (int)(e % a.width)]);
                 if (v < INFINITY) x = fmaxf(x, v);
@@ -958,12 +963,12 @@ int run_fit(mf_ctx *ctx, const mf_predictor *p, const float *d_on, int n, const 
     a.partial_step = f.step(g != nullptr);
     float *const ranges = ctx->fit_W1 + FOLD_RANGES;
     FitArgs folded = a;                                     // as wide_kernel takes it
-    // (predictions scale by every sample's own SM share)
-    const bool share_first = a.norm && a.W1sm && g, fallback = !f.wide && !a.norm, look = !f.wide && (!a.norm || share_first);
+    // What no norm bounds: features, and the SM share, but where there are no gradients, since there every sample is scaled by its own.
+    const bool look = !f.wide && (!a.norm || (a.W1sm && g));
     if (f.wide || look) {
         FoldArgs w{};
         w.W1 = p->d_W1; w.b1 = p->d_b1; w.g = p->d_ln_w; w.beta = p->d_ln_b;
-        w.F = p->F; w.padded = f.padded; w.half = f.half; w.rows_of_weights = f.wide || fallback ? f.H : 0;
+        w.F = p->F; w.padded = f.padded; w.half = f.half; w.rows_of_weights = f.H;
         w.W = ctx->fit_W1; w.bias = ctx->fit_W1 + FOLD_BIAS; w.ranges = ranges;
         w.width = a.norm ? 1 : p->F;
         for (int k = 0; k < 2; ++k) { w.X[k] = a.X[k]; w.index[k] = a.index[k]; w.rows[k] = a.rows[k]; w.first[k] = a.norm ? a.sm_feature[k] : 0; }
@@ -978,7 +983,7 @@ int run_fit(mf_ctx *ctx, const mf_predictor *p, const float *d_on, int n, const 
     }
     int rc = MF_OK;
     if (!f.wide) rc = f.H == 64 ? launch_fit_for<64>(ctx, a, f, g != nullptr) : launch_fit_for<128>(ctx, a, f, g != nullptr);
-    if (rc == MF_OK && (f.wide || fallback)) rc = mf_launch_wide(ctx, folded, f, ranges, g != nullptr);
+    if (rc == MF_OK && (f.wide || look)) rc = mf_launch_wide(ctx, folded, f, ranges, g != nullptr);
     if (rc != MF_OK || !a.partial) return rc;
     FitOut o{};
     if (g) {

@@ -79,3 +79,23 @@ def test_predictions_beside_a_large_sm_share(ctx, named, value, count, H):
         value64, bound = expected[name]
         assert (np.abs(got[name] - value64)[others] <= 1e-5 * value64[others]).all(), name
         ref.within(got[name][~others], value64[~others], bound[~others], name)
+
+
+@pytest.mark.parametrize("H", [64, 128])
+@pytest.mark.parametrize("count, n", [(40, 50), (20001, 50), (40, 500)])
+@pytest.mark.parametrize("value", [4e3, 1e9, 1e12])
+@pytest.mark.parametrize("which", ["unnamed", "half named", "named"])
+def test_a_fit_beside_a_large_sm_share(ctx, which, value, count, n, H):
+    """"half named": by samples that name no pair, as their other index is out of range."""
+    s = with_large_shares(72, count, H, value, n=n, missing=True)
+    if which == "half named":
+        s["on"][:2], s["off"][:2] = (7, -1), (-3, 9)
+    if which == "named":
+        s["on"][5], s["off"][5] = 7, 9
+    with np.errstate(over="ignore"):
+        s = close.away_from_kinks(s, (0.1, 2, 3))
+        assert which != "named" or s["on"][5] == 7
+        expected = close.room(s, (0.1, 2, 3), longest=count / 64)
+        close.check(call(ctx, s, (0.1, 2, 3)), expected)
+    alone = call(ctx, s, (0.1, 2, 3), want=False)
+    close.check(alone, {k: expected[k] for k in alone})
