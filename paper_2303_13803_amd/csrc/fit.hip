@@ -31,7 +31,8 @@
 // instructions reach 152; the matrix pipe is busy a third of that, and either kind of wavefront takes some 2000 cycles for each of the four
 // stages, its own chain of LDS reads, products and arithmetic.  2000 samples of 16 features through 64 units 19 us; 200,003 predictions 61.
 //
-// NaN: a ReLU that is one instruction turns it into 0, so what is not finite among the weights, or a sample's features, is added to the output as a NaN.
+// NaN: a ReLU that is one instruction turns it into 0, so what is not finite among the weights, or a sample's features, is added to the output as a NaN; its features are
+// 0 otherwise, so that a sample that has neither features nor a target changes no gradient.
 #include "fit_parts.h"
 
 typedef _Float16 half2v __attribute__((ext_vector_type(2)));
@@ -271,7 +272,7 @@ __global__ __launch_bounds__(H * 4, 2) void fit_kernel(const FitArgs a, const fl
         if (with_share) {
             const auto both = __builtin_amdgcn_permlane32_swap(__float_as_uint(next_share), __float_as_uint(next_share), false, false);
             const float share = fminf(1.0f - __uint_as_float(both[0]), __uint_as_float(both[1]));
-            if (hh == 0) sh.share[it & 3][nn] = named < 0 ? 0.0f : share;
+            if (hh == 0) sh.share[it & 3][nn] = named < 0 || !(share * 0.0f == 0.0f) ? 0.0f : share;
         }
         if (hh == 0) sh.real[to][nn] = named >= 0;
     };
@@ -626,6 +627,14 @@ __global__ __launch_bounds__(H * 4, 2) void fit_kernel(const FitArgs a, const fl
             sum += v[e];
         }
         sum = group_sum<UB>(sum);
+        // What is not finite is added to the output (`bad`) and has no other part: gradients sum up what is passed back, nothing where nothing was measured,
+        // times features.
+        const float bad = sum * 0.0f;
+        if (GRAD && !(bad == 0.0f)) {
+            sum = 0.0f;
+#pragma unroll
+            for (int e = 0; e < EACH; ++e) v[e] = 0.0f;
+        }
         if (a.norm) {
             float squares = 0.0f;
             mean = sum * inverse;
@@ -646,7 +655,7 @@ __global__ __launch_bounds__(H * 4, 2) void fit_kernel(const FitArgs a, const fl
             *(half4v *)((char *)&sh.xs[to][0] + place) = half4v{hi[e], hi[e + 1], hi[e + 2], hi[e + 3]};
             *(half4v *)((char *)&sh.xs[to][1] + place) = half4v{lo[e], lo[e + 1], lo[e + 2], lo[e + 3]};
         }
-        if (sub == 0) sh.bad[to][side][own] = sum * 0.0f;
+        if (sub == 0) sh.bad[to][side][own] = bad;
     };
     const unsigned short limit = (unsigned short)(rule.limit - 1);      // (a dropout's limit is at least 1)
     const ushort2v below = {limit, limit};

@@ -16,7 +16,7 @@ template <int H>
 constexpr size_t wide_lds_bytes(bool grad)
 {
     return sizeof(float) * ((size_t)H * (H + 4) + FIT_ROWS * (FIT_CHUNK + 4) + (size_t)FIT_ROWS * (H + 4) * (grad ? 2 : 1) +
-                            2 * (H / 32) * FIT_ROWS + FIT_ROWS * 5 + 4 * FIT_ROWS + 5 * H);
+                            2 * (H / 32) * FIT_ROWS + FIT_ROWS * 6 + 4 * FIT_ROWS + 5 * H);
 }
 
 template <int H, int GT, bool GRAD>
@@ -34,7 +34,8 @@ __global__ __launch_bounds__(H * 4) void wide_kernel(const FitArgs a, const floa
     float *part = back + (GRAD ? T * PITCH : 0), *target = part + 2 * UB * T, *target_slow = target + T, *share = target_slow + T;
     int *at_on = (int *)(share + T), *at_off = at_on + T;
     float2 *moments = (float2 *)(at_off + T);
-    float *vec = (float *)(moments + 2 * T);                // b1, b2, W3, W3 of the slowdown unit, W1sm
+    float *bad = (float *)(moments + 2 * T);                // with gradients: NaN where a sample's features are not finite, which are 0 then (see fit.hip)
+    float *vec = bad + T;                                   // b1, b2, W3, W3 of the slowdown unit, W1sm
     const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6, nn = lane & 31, hh = lane >> 5;
     const int ub = wave % UB, sh = wave / UB;               // units 32 ub .. and samples 32 sh .. of the forward pass are this wavefront's
     const int unit = 32 * ub + tile_unit(nn), mine = 32 * sh + nn, u0 = 32 * ub + 8 * hh;
@@ -81,13 +82,21 @@ __global__ __launch_bounds__(H * 4) void wide_kernel(const FitArgs a, const floa
         }
     };
     auto lay = [&](const int chunk) {
+        unsigned not_finite = 0;
         const int c = chunk * FIT_CHUNK + tid % FIT_CHUNK, side = c >= a.half, f = c - side * a.half;
 #pragma unroll
         for (int k = 0; k < EACH_FEATURE; ++k) {
             const int s = tid / FIT_CHUNK + k * (THREADS / FIT_CHUNK);
             const float2 m = moments[2 * s + side];
-            xs[s * XP + tid % FIT_CHUNK] = f < a.F && at_on[s] >= 0 ? (feature[k] - m.x) * m.y : 0.0f;
+            const float v = f < a.F && at_on[s] >= 0 ? (feature[k] - m.x) * m.y : 0.0f;
+            const bool finite = !GRAD || fabsf(v) < INFINITY;
+            xs[s * XP + tid % FIT_CHUNK] = finite ? v : 0.0f;
+            not_finite |= finite ? 0u : 1u << k;
         }
+        if (GRAD && not_finite)
+#pragma unroll 1
+            for (int k = 0; k < EACH_FEATURE; ++k)
+                if (not_finite >> k & 1u) bad[tid / FIT_CHUNK + k * (THREADS / FIT_CHUNK)] = __builtin_nanf("");
     };
     // bias, ReLU and dropout of this lane's 16 units of one layer
     auto activate = [&](const floatx16 &z, float (&h)[16], const float *bias, const float share_here, long long sample, unsigned layer) {
@@ -132,7 +141,13 @@ __global__ __launch_bounds__(H * 4) void wide_kernel(const FitArgs a, const floa
             const float none = __builtin_nanf("");
             target[tid] = i >= 0 && a.target[0] ? a.target[0][s] : none;
             target_slow[tid] = i >= 0 && a.target[1] ? a.target[1][s] : none;
-            share[tid] = i >= 0 && a.W1sm ? fminf(1.0f - a.X[0][(size_t)i * a.F + a.sm_feature[0]], a.X[1][(size_t)j * a.F + a.sm_feature[1]]) : 0.0f;
+            float at = i >= 0 && a.W1sm ? fminf(1.0f - a.X[0][(size_t)i * a.F + a.sm_feature[0]], a.X[1][(size_t)j * a.F + a.sm_feature[1]]) : 0.0f;
+            bad[tid] = 0.0f;
+            if (GRAD && !(at * 0.0f == 0.0f)) {
+                at = 0.0f;
+                bad[tid] = none;
+            }
+            share[tid] = at;
         }
         __syncthreads();
         fetch(0);
@@ -208,7 +223,7 @@ __global__ __launch_bounds__(H * 4) void wide_kernel(const FitArgs a, const floa
         zs = both_halves(zs);
         if (hh == 0) { part[ub * T + mine] = zp; part[(UB + ub) * T + mine] = zs; }
         __syncthreads();
-        zp = b3; zs = b3s;
+        zp = b3 + bad[mine]; zs = b3s + bad[mine];
 #pragma unroll
         for (int k = 0; k < UB; ++k) { zp += part[k * T + mine]; zs += part[(UB + k) * T + mine]; }
         const float y = 1.0f / (1.0f + expf(-zp)), ys = 1.0f / (1.0f + expf(-zs));

@@ -99,3 +99,40 @@ def test_a_fit_beside_a_large_sm_share(ctx, which, value, count, n, H):
         close.check(call(ctx, s, (0.1, 2, 3)), expected)
     alone = call(ctx, s, (0.1, 2, 3), want=False)
     close.check(alone, {k: expected[k] for k in alone})
+
+
+# ---- features that are not there, of samples whose targets are not there either
+
+@pytest.mark.parametrize("H", [64, 128])
+@pytest.mark.parametrize("F", [16, 40, 100])
+@pytest.mark.parametrize("norm", [False, True])
+@pytest.mark.parametrize("value", [np.nan, np.inf])
+@pytest.mark.parametrize("large", [False, True])
+def test_features_nobody_has_measured(ctx, large, value, norm, F, H):
+    """A workload without metrics, in pairs nobody has measured: the loss and gradients are those without these samples to the bit; their
+    predictions are NaN.  large: also through float32 products, where there is no norm."""
+    s = problem(73, 700, F, H, norm=norm, sm=True, slow=True, missing=True)
+    if large:
+        s["x_off"][3, 4] = 1e5
+        s["params"]["W1"][:, F + 4] /= np.float32(1e5)
+    s["x_on"][7] = value
+    s["x_off"][9, 2:] = value
+    blank = ((s["on"] == 7) | (s["off"] == 9)) & (s["on"] >= 0) & (s["off"] < 40)
+    assert blank.any()
+    s["target"][blank], s["target_slow"][blank] = np.nan, np.nan
+    got = call(ctx, s, (0.1, 2, 3))
+    without = call(ctx, dict(s, on=np.where(blank, -1, s["on"]).astype(np.int32)), (0.1, 2, 3))
+    assert np.isnan(got["sigma"][blank]).all() and np.isnan(got["sigma_slow"][blank]).all()
+    assert (got["sigma"][~blank] == without["sigma"][~blank]).all()
+    same_bits(got, without, [k for k in got if not k.startswith("sigma")])
+    assert all(np.isfinite(got[k]).all() for k in s["params"])
+
+
+@pytest.mark.parametrize("F", [16, 100])
+@pytest.mark.parametrize("norm", [False, True])
+def test_features_that_are_not_finite_show_where_something_was_measured(ctx, norm, F):
+    s = problem(74, 300, F, 64, norm=norm)
+    s["x_on"][7] = np.nan
+    assert (s["on"] == 7).any()
+    got = call(ctx, s)
+    assert np.isnan(got["loss"]).all() and all(np.isnan(got[k]).any() for k in ("W3", "b3", "W2", "b2", "W1", "b1"))
