@@ -31,8 +31,8 @@
 // instructions reach 152; the matrix pipe is busy a third of that, and either kind of wavefront takes some 2000 cycles for each of the four
 // stages, its own chain of LDS reads, products and arithmetic.  2000 samples of 16 features through 64 units 19 us; 200,003 predictions 61.
 //
-// NaN: a ReLU that is one instruction turns it into 0, so what is not finite among the weights, or a sample's features, is added to the output as a NaN; its features are
-// 0 otherwise, so that a sample that has neither features nor a target changes no gradient.
+// NaN: a ReLU that is one instruction turns it into 0, so what is not finite among the weights, their bounds, or a sample's features is added to the output as a NaN; its
+// features are 0 otherwise, so that a sample that has neither features nor a target changes no gradient.
 #include "fit_parts.h"
 
 typedef _Float16 half2v __attribute__((ext_vector_type(2)));
@@ -50,13 +50,12 @@ constexpr int FIT_ROWS = 32;
 // The exponent of the largest power of two that takes a value of at most `bound` to below 2^14 (0 for bounds that are none).
 __device__ __forceinline__ int exponent_below(float bound)
 {
-    if (!(bound > 0.0f) || bound > 1e30f) return 0;
+    if (!(bound > 0.0f) || !(bound < INFINITY)) return 0;
     int e;
     (void)frexpf(bound, &e);                                // bound < 2^e
-    e = e < -96 ? -96 : e > 96 ? 96 : e;
+    e = e < -96 ? -96 : e;
     return 14 - e;
 }
-__device__ __forceinline__ float scale_below(float bound) { return ldexpf(1.0f, exponent_below(bound)); }
 
 // v = hi + lo in fp16, to 22 bits.  The remainder is exact; written as a fused multiply-add by a -1 that the optimiser cannot see it is one
 // instruction that reads the fp16 piece itself.
@@ -356,7 +355,8 @@ __global__ __launch_bounds__(H * 4, 2) void fit_kernel(const FitArgs a, const fl
         sum = both_halves(sum);
         bias1 = a.b1[unit] + both_halves(more);
         const float w_share = with_share ? a.W1sm[unit] : 0.0f;
-        v[7] = fabsf(bias1) + fabsf(w_share) + (a.norm ? sqrtf(both_halves(squares)) * length * 1.42f : 0.0f);
+        // (|u|_2 <= sqrt(F) on either side, so no entry is more; squares of weights beyond 1.8e19 are no float32)
+        v[7] = fabsf(bias1) + fabsf(w_share) + (a.norm ? fminf(sqrtf(both_halves(squares)) * length * 1.42f, sum * length * 1.001f) : 0.0f);
         v[8] = fabsf(w_share) + (a.norm ? 0.0f : sum);
         float column = 0.0f;
 #pragma unroll
@@ -417,16 +417,19 @@ __global__ __launch_bounds__(H * 4, 2) void fit_kernel(const FitArgs a, const fl
         for (int q = 0; q < 9; ++q) v[q] = fmaxf(v[q], sh.most[q][x]);
         poison += sh.most[9][x];
     }
-    const float s_x = scale_below(a.norm ? length * 1.001f : v[1]), s_w2 = scale_below(v[4]), s_w1 = scale_below(v[5]);
+    const int e_x = exponent_below(a.norm ? length * 1.001f : v[1]), e_w2 = exponent_below(v[4]), e_w1 = exponent_below(v[5]);
     const float bound2 = 0.5f * (1.0f + v[0]) * (v[2] + v[3]) * factor * 1.001f;
-    const float s_dz2 = scale_below(bound2), s_dz1 = scale_below(bound2 * factor * v[6] * 1.001f);
+    const int e_dz2 = exponent_below(bound2), e_dz1 = exponent_below(bound2 * factor * v[6] * 1.001f);
     // Without gradients a lane of the forward wavefronts has a sample of its own, whose SM share, where nothing bounds it, scales what is its own and
     // nobody else's (OWN: then by_z1, by_z2, sh.b1 and sh.wsm lack that scale).
     constexpr bool OWN = !GRAD && EXTRA;
-    const float s_d1 = OWN ? 1.0f : scale_below((v[7] + v[8] * v[1]) * factor * 1.001f);
-    const float most_d1 = (v[7] + (a.norm ? 0.0f : v[8] * v[1])) * factor * 1.001f, most_share = a.norm ? v[8] * factor * 1.001f : 0.0f;
+    const float most_d1 = (v[7] + (OWN && a.norm ? 0.0f : v[8] * v[1])) * factor * 1.001f, most_share = a.norm ? v[8] * factor * 1.001f : 0.0f;
+    const int e_d1 = OWN ? 0 : exponent_below(most_d1);
     // what accumulators of the three products are multiplied with
-    const float by_z1 = factor * s_d1 / (s_x * s_w1), by_z2 = factor / (s_d1 * s_w2), by_d1 = factor * s_dz1 / (s_dz2 * s_w2), by_dz = factor * s_dz2;
+    // (exponents are added up first: products of scales may be no float32)
+    const float by_z1 = ldexpf(factor, e_d1 - e_x - e_w1), by_z2 = ldexpf(factor, -e_d1 - e_w2), by_d1 = ldexpf(factor, e_dz1 - e_dz2 - e_w2), by_dz = ldexpf(factor, e_dz2);
+    const float s_x = ldexpf(1.0f, e_x), s_w1 = ldexpf(1.0f, e_w1), s_w2 = ldexpf(1.0f, e_w2), s_d1 = ldexpf(1.0f, e_d1);
+    poison += most_d1 * v[4] * 0.0f;                        // NaN where even a bound on layer 2's terms is none
     if (tid < H) {
         sh.wsm[tid] = with_share ? a.W1sm[tid] * (factor * s_d1) : 0.0f;
         sh.b2[tid] = a.b2[tid] * factor;
@@ -502,7 +505,8 @@ __global__ __launch_bounds__(H * 4, 2) void fit_kernel(const FitArgs a, const fl
                 for (int b = 0; b < XB; ++b) z = product(w1[b], x[b], b == 0 ? zero : z);
             }
             float share = with_share ? sh.share[it & 3][nn] : 0.0f;
-            const int own_scale = OWN ? exponent_below(fmaf(most_share, fabsf(share), most_d1)) : 0;
+            const float own_most = fmaf(most_share, fabsf(share), most_d1);
+            const int own_scale = OWN ? exponent_below(own_most) : 0;
             const float s_own = ldexpf(1.0f, own_scale), by_z1_here = OWN ? by_z1 * s_own : by_z1, by_z2_here = OWN ? ldexpf(by_z2, -own_scale) : by_z2;
             if (OWN) share *= s_own;
 #pragma unroll
@@ -548,6 +552,7 @@ __global__ __launch_bounds__(H * 4, 2) void fit_kernel(const FitArgs a, const fl
             // (with two output units either half of the wavefront takes one)
             const int unit3 = EXTRA && slow ? hh : 0;
             float z3 = b3 + sh.bad[now][0][nn] + sh.bad[now][1][nn];
+            if (OWN) z3 += own_most * v[4] * 0.0f;
 #pragma unroll
             for (int k = 0; k < UB; ++k) z3 += sh.part[unit3][k][nn];
             const float y = 1.0f / (1.0f + expf(-z3));
@@ -790,7 +795,7 @@ __global__ __launch_bounds__(H * 4, 2) void fit_kernel(const FitArgs a, const fl
     if (!GRAD || !out) return;
     if (L::D1 > 1) add_w2((mine + 1) & 1, 1, [] {});
     add_w1(mine - 1, [] {});
-    const float by2 = 1.0f / (s_dz2 * s_d1), by1 = 1.0f / (s_dz1 * s_x);
+    const float by2 = ldexpf(1.0f, -e_dz2 - e_d1), by1 = ldexpf(1.0f, -e_dz1 - e_x);
 #pragma unroll
     for (int e = 0; e < 16; ++e) {
         const int k = 32 * ub + 8 * (e >> 2) + 4 * hh + (e & 3);
@@ -799,9 +804,9 @@ __global__ __launch_bounds__(H * 4, 2) void fit_kernel(const FitArgs a, const fl
 #pragma unroll
         for (int t = 0; t < CT; ++t) out[S::G + k * (32 * CT) + 32 * t + nn] = gw1[t][e] * by1;
     }
-    gb1 = both_halves(gb1) / s_dz1;
-    gb2 = both_halves(gb2) / s_dz2;
-    gsm = EXTRA ? both_halves(gsm) / s_dz1 : 0.0f;
+    gb1 = ldexpf(both_halves(gb1), -e_dz1);
+    gb2 = ldexpf(both_halves(gb2), -e_dz2);
+    gsm = EXTRA ? ldexpf(both_halves(gsm), -e_dz1) : 0.0f;
     if (hh == 0) {
         out[S::B1 + 32 * ub + nn] = gb1;
         out[S::B2 + 32 * ub + nn] = gb2;

@@ -136,3 +136,36 @@ def test_features_that_are_not_finite_show_where_something_was_measured(ctx, nor
     assert (s["on"] == 7).any()
     got = call(ctx, s)
     assert np.isnan(got["loss"]).all() and all(np.isnan(got[k]).any() for k in ("W3", "b3", "W2", "b2", "W1", "b1"))
+
+
+# ---- weights of any size
+
+@pytest.mark.parametrize("H", [64, 128])
+@pytest.mark.parametrize("size", [1e25, 1e32, 1e36])
+@pytest.mark.parametrize("which", ["W1", "W2"])
+def test_predictions_with_weights_of_any_size(ctx, which, size, H):
+    """Predictions are then certain; they are what they are by themselves, where few pairs are asked for."""
+    s = problem(75, 5000, 16, H)
+    s["params"][which] *= np.float32(size)
+    if which == "W1":
+        s["params"]["W2"] *= np.float32(1e-30)
+    with np.errstate(over="ignore"):
+        value, bound = definition(s)["sigma"]
+    got = predictions(ctx, s)["sigma"]
+    few = np.concatenate([predictions(ctx, dict(s, on=s["on"][k:k + 1000], off=s["off"][k:k + 1000]))["sigma"] for k in range(0, 5000, 1000)])
+    # (exp(-z) beyond 2^128 is an infinity, and the prediction 0 where it is below 2^-128)
+    ref.within(few, value, bound + 2.0 ** -128, "few")
+    ref.within(got, value, bound + 2.0 ** -128, "many")
+
+
+@pytest.mark.parametrize("H", [64, 128])
+@pytest.mark.parametrize("w2, w3", [(1e-13, 1e-20), (1e-20, 1e-12), (1e-6, 1e-22)])
+def test_gradients_through_weights_of_next_to_nothing(ctx, w2, w3, H):
+    """Their products are far above the smallest numbers there are, also where scales to fp16's range would not be."""
+    s = problem(76, 300, 16, H)
+    s["params"]["W2"] *= np.float32(w2)
+    s["params"]["W3"] *= np.float32(w3)
+    s = close.away_from_kinks(s, margin=0.0)
+    got, expected = call(ctx, s, None, 1.0), close.room(s, None, 1.0, longest=10)
+    # (the second layer's bias decides which of its units are open)
+    close.check(got, {k: expected[k] for k in ("W1", "b1", "W2", "b2", "ln_w", "ln_b")})
