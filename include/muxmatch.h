@@ -124,7 +124,7 @@ typedef struct {
     float   slow_limit;         /* pairs predicted above it are infeasible              */
     const float *d_ln_w;        /* [2F] or NULL: weight of the norm of the features     */
     const float *d_ln_b;        /* [2F]  (with d_ln_w)                                  */
-    float   ln_eps;             /* > 0                                                  */
+    float   ln_eps;             /* >= 2^-126                                            */
 } mf_predictor;
 
 /* Filled on the host by the solving calls. */

@@ -1,5 +1,6 @@
 // C entry points: argument checks, context life cycle, stage timing.
 #include "internal.h"
+#include <float.h>
 #include <math.h>
 #include <stdlib.h>
 #include <string.h>
@@ -27,7 +28,8 @@ int mf_check_predictor(const mf_predictor *p)
     if (p->d_W1sm && (!aligned16(p->d_W1sm) || p->sm_on_feature < 0 || p->sm_on_feature >= p->F ||
                       p->sm_off_feature < 0 || p->sm_off_feature >= p->F))
         return MF_ERR_ARG;
-    if (p->d_ln_w && (!p->d_ln_b || !(p->ln_eps > 0.0f) || isinf(p->ln_eps))) return MF_ERR_ARG;
+    // (below the smallest normal number the root of a row of equal features is one that the fit's reciprocal root does not take)
+    if (p->d_ln_w && (!p->d_ln_b || !(p->ln_eps >= FLT_MIN) || isinf(p->ln_eps))) return MF_ERR_ARG;
     return MF_OK;
 }
 
