@@ -321,16 +321,17 @@ class Context:
         with norm_eps also ln_w [2F], ln_b [2F], weight and bias of the layer norm of the features."""
         H = params["b1"].numel()
         F = params["W1"].shape[1] // 2
-        p = Predictor(F, H, float(scale), int(mem_feature), float(mem_limit),
-                      *[_ptr(params[k], torch.float32) for k in ("W1", "b1", "W2", "b2", "W3", "b3")],
-                      _ptr(params["W1sm"], torch.float32) if sm is not None else None,
-                      0 if sm is None else int(sm[0]), 0 if sm is None else int(sm[1]),
-                      _ptr(params["W3slow"], torch.float32) if slow_limit is not None else None,
-                      _ptr(params["b3slow"], torch.float32) if slow_limit is not None else None,
-                      0.0 if slow_limit is None else float(slow_limit),
-                      _ptr(params["ln_w"], torch.float32) if norm_eps is not None else None,
-                      _ptr(params["ln_b"], torch.float32) if norm_eps is not None else None,
-                      0.0 if norm_eps is None else float(norm_eps))
+        there = {"d_W1sm": sm, "d_W3_slow": slow_limit, "d_b3_slow": slow_limit, "d_ln_w": norm_eps, "d_ln_b": norm_eps}
+        p = Predictor(F, H, float(scale), int(mem_feature), float(mem_limit))
+        for member, name, (columns, units, ones, squares, both) in PARAMETERS:
+            if there.get(member, params) is not None:
+                setattr(p, member, self._flat(params[name], torch.float32, columns * F + units * H + ones + squares * H * H + both * F * H, name))
+        if sm is not None:
+            p.sm_on_feature, p.sm_off_feature = int(sm[0]), int(sm[1])
+        if slow_limit is not None:
+            p.slow_limit = float(slow_limit)
+        if norm_eps is not None:
+            p.ln_eps = float(norm_eps)
         p._keep = params
         return p
 
