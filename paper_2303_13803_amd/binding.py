@@ -264,6 +264,8 @@ class Context:
     def dropout(self, x, y, p, seed, step=0, layer=0):
         """y = dropout of x, the mask made from (seed, step, layer, element); on a gradient, the backward pass.
         step: a number, or an int64 tensor of one value on the device.  y may be x."""
+        if not 0 <= layer < 65536:                          # (would reach the library without its upper bits)
+            raise MuxmatchError(ERR_ARG, "layer")
         kind, number, shape, px, ldx = self._matrix(x, "x")
         py, ldy = self._rows(y, kind, shape, "y")
         rows, width = shape
@@ -275,6 +277,8 @@ class Context:
         if len(shape) != 2 or shape[1] != F:
             raise ValueError(f"{what}: expected a matrix of {F} features a workload")
         rows = shape[0]
+        if rows > 0x7fffffff:                               # (would reach the library without its upper bits)
+            raise ValueError(f"{what}: expected fewer than 2^31 workloads")
         return self._flat(x, torch.float32, rows * F, what), rows
 
     def predictor_loss_work(self, pred, count):

@@ -54,3 +54,15 @@ def test_parameters_of_other_sizes(name):
 def test_parameters_of_other_kinds_and_places(change):
     with pytest.raises(TypeError):
         _host_context().predictor({**_params(), **change}, 1.0, sm=(1, 2), slow_limit=0.5, norm_eps=1e-5)
+
+
+def test_numbers_that_lose_their_upper_bits_on_the_way():
+    """2^32 + 5 workloads are not five, and layer 2^32 + 1 is not layer 1."""
+    from paper_2303_13803_amd import MuxmatchError
+    c = _host_context()
+    with pytest.raises(ValueError, match="x_on"):
+        c._side(torch.empty((2 ** 32 + 5, 1), device="meta"), 1, "x_on")
+    x = torch.zeros(3, 8)
+    for layer in (2 ** 32 + 1, -1, 65536):
+        with pytest.raises(MuxmatchError, match="layer"):
+            c.dropout(x, x, 0.5, 1, layer=layer)
