@@ -14,8 +14,8 @@
 // (|v - hi - lo| <= 2^-22 |v|), and a product is hi hi + hi lo + lo hi, added up in float32: three fp16 products at sixteen times
 // the rate of the float32 ones (2300 and 152 TFLOP/s measured).  fp16's range is seen to by scaling each operand with a power of two
 // from a bound on it that is never exceeded, to below 2^14; what is within 2^-17 of the bound keeps all its 22 bits, smaller
-// values lose absolute precision of 2^-39 of the bound.  The bounds: a normalised row has |u|_2 <= sqrt(F), so |z1_k| <= |W1_k|_2
-// sqrt(2F) + |b1_k|; |dz3| <= (1 + max |t|) / 2; and through W3 and W2 by their largest values and columns' sums.  Features that no norm
+// values lose absolute precision of 2^-39 of the bound.  The bounds: a normalised row has |u|_2 <= sqrt(F), so z1_k <= |W1_k|_2
+// sqrt(2F) + b1_k, and what is below 0 is not passed on; |dz3| <= (1 + max |t|) / 2; and through W3 and W2 by their largest values and columns' sums.  Features that no norm
 // bounds, those of an SM share behind a norm among them, are looked for; where one is above FIT_LARGEST all of it is done once more in float32 products
 // (wide_kernel), so that what others keep does not depend on it.  Without gradients a sample is scaled by its own SM share instead.
 //
@@ -298,7 +298,7 @@ __global__ __launch_bounds__(H * 4, 2) void fit_kernel(const FitArgs a, const fl
     // ---- bounds, and the scales that follow.  Weights are read as the operands that the forward wavefronts make of them: layer 1's with the
     // norm's weight, W2's transpose (or, without a way back, W2), a unit's in two lanes.
     float w[KB][8], u1[XB][8], bias1 = 0.0f, poison = 0.0f;
-    // largest of: targets, features (or, of those that a norm bounds, the SM share's two), output weights of either unit, weights of layers 2 and 1, columns' sums of W2, z1 without features and for each
+    // largest of: targets, features (or, of those that a norm bounds, the SM share's two), output weights of either unit, weights of layers 2 and 1, columns' sums of W2, z1 (not below 0) without features and for each
     float v[9] = {0.0f, 0.0f, 0.0f, 0.0f, 0.0f, 0.0f, 0.0f, 0.0f, 0.0f};
     const float length = sqrtf((float)a.F);
     const auto read_w2 = [&](const int b, float (&to)[8]) {
@@ -356,7 +356,9 @@ __global__ __launch_bounds__(H * 4, 2) void fit_kernel(const FitArgs a, const fl
         bias1 = a.b1[unit] + both_halves(more);
         const float w_share = with_share ? a.W1sm[unit] : 0.0f;
         // (|u|_2 <= sqrt(F) on either side, so no entry is more; squares of weights beyond 1.8e19 are no float32)
-        v[7] = fabsf(bias1) + fabsf(w_share) + (a.norm ? fminf(sqrtf(both_halves(squares)) * length * 1.42f, sum * length * 1.001f) : 0.0f);
+        const float rest = fabsf(w_share) + (a.norm ? fminf(sqrtf(both_halves(squares)) * length * 1.42f, sum * length * 1.001f) : 0.0f);
+        // what the ReLU passes on: a bias that closes the unit lowers it (and rounds what is added to it)
+        v[7] = fmaxf(bias1 + rest + 1e-6f * (fabsf(bias1) + rest), 0.0f);
         v[8] = fabsf(w_share) + (a.norm ? 0.0f : sum);
         float column = 0.0f;
 #pragma unroll

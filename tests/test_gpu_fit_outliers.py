@@ -169,3 +169,20 @@ def test_gradients_through_weights_of_next_to_nothing(ctx, w2, w3, H):
     got, expected = call(ctx, s, None, 1.0), close.room(s, None, 1.0, longest=10)
     # (the second layer's bias decides which of its units are open)
     close.check(got, {k: expected[k] for k in ("W1", "b1", "W2", "b2", "ln_w", "ln_b")})
+
+
+@pytest.mark.parametrize("H", [64, 128])
+@pytest.mark.parametrize("norm, sm", [(True, True), (True, False), (False, True)])
+@pytest.mark.parametrize("bias", [-1e9, -1e20, -3e38])
+def test_units_closed_by_their_bias(ctx, bias, norm, sm, H):
+    """However far: the others' values are scaled by what units can pass on, not by what closes some."""
+    s = problem(77, 5000, 16, H, norm=norm, sm=sm)
+    s["params"]["b1"][[3, 40]] = bias
+    s = close.away_from_kinks(s, (0.1, 2, 3))
+    expected = close.room(s, (0.1, 2, 3), longest=80)
+    got = call(ctx, s, (0.1, 2, 3))
+    close.check(got, expected)
+    alone = call(ctx, s, (0.1, 2, 3), want=False)
+    close.check(alone, {k: expected[k] for k in alone})
+    exact = close.evaluate(s)[0]["sigma"]
+    assert (np.abs(predictions(ctx, s)["sigma"] - exact) <= 1e-5 * exact).all()
