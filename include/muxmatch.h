@@ -103,6 +103,8 @@ typedef struct mf_ctx mf_ctx;
  * [0,F) of the two vectors for the online and [F,2F) for the offline one.
  * The memory fraction and the SM share are taken from the features as they are.
  * All parameter pointers are DEVICE pointers to float32, row-major.
+ * Start from a struct of zeros: members may be added behind the last, zero for "without", and
+ * a program is built with the header of the library that it runs with.
  */
 typedef struct {
     int32_t F;                  /* features per workload (1..256)                       */
@@ -486,8 +488,21 @@ typedef struct {
  * d_sigma and d_sigma_slow ([count], either may be NULL) receive the predictions, with the same dropout; 0 for a
  * sample that names no pair.  Gradients are sums in a fixed order: the same call gives the same bits.
  * A ReLU passes no gradient at 0.  d_work as in mf_layer_norm_grad.  What is written must not overlap what is read.
- * Products take float32 operands to 22 bits or, of weights, features behind a norm and what is passed back, to 2^-39 of the largest of
- * their kind in the call where that is more, and are added up in float32.
+ * Products take float32 operands to 22 bits and are added up in float32.  Operands that are small beside others of their kind are taken to
+ * 2^-39 of a bound on these instead:
+ *   weights of a layer       the largest of them (of the first, times the norm's weight)
+ *   features                 sqrt(F) behind a norm; else the largest feature of the call, of all workloads or of those that samples name
+ *   first layer's units      the most that one of them can pass on: b1 (and W1 times the norm's bias) + |row of W1| sqrt(2F) behind a norm,
+ *                            else b1 + sum |row of W1| times that feature; and |W1sm| times 1 + the largest feature of an SM share (without
+ *                            gradients: 1 + the sample's own share)
+ *   passed back to layer 2   (1 + T) / 2 times the largest |W3| (of both units, added up), T the largest |target| among the samples of a
+ *                            workgroup that name a pair, 1 at least; to layer 1: that times the largest column sum of |W2|
+ * (units and what is passed back times the dropout's factor).  With more than 64 features, and where a feature that no norm bounds (the SM share's two
+ * among them) is above 4096, operands are float32.  Biases' gradients, and W1sm's, are sums of what is passed back as it is taken there.
+ * Sums of squares are float32 too: a norm is one up to differences of 1e18.  Where what bounds a layer is no float32 (a NaN or an infinity
+ * among the weights, weights near 1e38), predictions and the loss are NaN.
+ * A sample with a feature that is not finite makes its prediction a NaN, and the loss and gradients where a target of it was measured; where none was, it has
+ * no part in either.
  * scale, mem_feature, mem_limit and slow_limit of the predictor play no part but have to be valid.
  */
 int64_t mf_predictor_loss_work(mf_ctx *ctx, const mf_predictor *pred, int64_t count);

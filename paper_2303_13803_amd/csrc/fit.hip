@@ -27,12 +27,15 @@
 //     sums      dW2, second half     G                    next features    dW2, first half      (either half: 16 samples)
 // so that the matrix pipe has something to do throughout; random bits for the next samples are drawn in all four stages.
 //
-// Measured: a million samples of 32 features a workload through 128 units, with every option, 0.51 ms, 263 TFLOP/s where float32's matrix
+// Measured: a million samples of 32 features a workload through 128 units, with every option, 0.50 ms, 268 TFLOP/s where float32's matrix
 // instructions reach 152; the matrix pipe is busy a third of that, and either kind of wavefront takes some 2000 cycles for each of the four
-// stages, its own chain of LDS reads, products and arithmetic.  2000 samples of 16 features through 64 units 19 us; 200,003 predictions 61.
+// stages, its own chain of LDS reads, products and arithmetic.  2000 samples of 16 features through 64 units 18 us; 200,003 predictions 60,
+// the loss alone of as many 67; a million samples without a norm 0.49 ms, 2000 of them 20 us (the launches that look for what is too large, and that find nothing,
+// 5 and 1 to 4).  Registers do not suffice for what a pass with gradients keeps: the compiler leaves 82 vector registers of 256 in memory with 32 features and 128 units,
+// 182 with 64; without gradients none up to 48 features.
 //
-// NaN: a ReLU that is one instruction turns it into 0, so what is not finite among the weights, their bounds, or a sample's features is added to the output as a NaN; its
-// features are 0 otherwise, so that a sample that has neither features nor a target changes no gradient.
+// NaN: a ReLU that is one instruction turns it into 0, so what is not finite among the weights, their bounds, or a sample's features is
+// added to the output as a NaN; its features are 0 otherwise, so that a sample that has neither features nor a target changes no gradient.
 #include "fit_parts.h"
 
 typedef _Float16 half2v __attribute__((ext_vector_type(2)));
@@ -973,7 +976,7 @@ int run_fit(mf_ctx *ctx, const mf_predictor *p, const float *d_on, int n, const 
     a.drop = rule && rule->limit > 0;
     if (a.drop) { a.rule = *rule; a.step = (const unsigned long long *)d_step; }
     // Predictions that the device holds at once, a workgroup each (2048 threads a compute unit, 4 H a pair), without staging and looking for bounds: one of 32 features and
-    // 128 units 3.5 us, with them 10.6; 1024 8.3 and 10.9; 2048 14.2 and 11.0.  With 16 and 64: 3.1 and 7.5; 2048 6.5 and 7.9; 4096 10.3 and 7.9.
+    // 128 units 3.5 us, with them 9.7; 1024 8.4 and 10.0; 2048 14.5 and 10.1.  With 16 and 64: 3.2 and 6.3; 2048 6.4 and 6.5; 4096 10.3 and 6.6.
     if (!d_work && a.count <= (ctx->n_cus > 0 ? ctx->n_cus : 256) * (512ll / f.H)) return mf_launch_few(ctx, a, f.H);
     a.partial = (float *)d_work;
     a.partial_step = f.step(g != nullptr);

@@ -8,7 +8,7 @@
 typedef float floatx16 __attribute__((ext_vector_type(16)));
 
 // Features a workload from which on fit_wide.hip takes over: as many as fit_kernel has accumulators and LDS for.  With 64, 100,000 samples and 128 units it took
-// 439 us and fit_kernel takes 151; with 64 units 278 and 142.
+// 382 us and fit_kernel takes 135; with 64 units 226 and 116.
 constexpr int FIT_WIDE_FROM = 65;
 // Features of a predictor without a norm, and those of an SM share, go to fp16 pieces up to this size: what one of them may be, all samples of a call are scaled by, and the
 // bits that are left for a z1 of about 1 are then still those of float32.

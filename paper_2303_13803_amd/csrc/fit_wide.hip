@@ -1,8 +1,8 @@
 // The pass over the samples in float32 products: of predictors of many features (65 to 256 a workload), and where a feature that no norm
 // bounds is too large for pieces (FIT_LARGEST).  Features are staged 64 columns at a time, twice a sample, and gradients of layer 1 are kept for 256 columns at a
 // time, which is as many as there are accumulators for: more take another pass over the samples each.  See fit.hip for what is computed.
-// Measured with 128 units: 100,000 samples of 65 features 0.54 ms (31 TFLOP/s; float32's matrix instructions reach 152), 30,000 of 256 0.50; bound by waits
-// between its stages, with one workgroup a compute unit.
+// Measured with 128 units: 100,000 samples of 65 features 0.48 ms (35 TFLOP/s; float32's matrix instructions reach 152), 30,000 of 256 0.47, 200,003 predictions of 100
+// 0.31; bound by waits between its stages, with one workgroup a compute unit (LDS lets no second one in), and with 91 vector registers in memory.
 #include "fit_parts.h"
 
 namespace {
